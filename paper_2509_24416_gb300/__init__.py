@@ -5,4 +5,4 @@ C ABI (include/clq.h), with a ctypes binding in ``clq``.
 Importing the package does not load the CUDA library; the first call into
 ``clq`` does, and raises if libclq.so has not been built.
 """
-__all__ = ["clq", "synth", "build"]
+__all__ = ["clq", "mx", "synth", "build"]

@@ -483,6 +483,8 @@ int32_t fused_linear_check(const void* X, int32_t dtype, int32_t M, int32_t K, i
   return check_e2m3(w_codes, K, W);
 }
 
+int32_t device_status(int32_t** status) { return device_setup(status); }
+
 int32_t device_check() {
   int32_t* status = nullptr;
   return device_setup(&status);

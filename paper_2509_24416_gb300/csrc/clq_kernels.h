@@ -119,6 +119,8 @@ int32_t fused_linear_check(const void* X, int32_t dtype, int32_t M, int32_t K, i
                            const float* s_w, const void* bias, int32_t N, const void* Y,
                            bool* noop);
 int32_t device_check();
+// The same check, and the address of the device status word.
+int32_t device_status(int32_t** status);
 
 // Bounded-wait self test (one CTA, one mbarrier nothing arrives at).
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, int32_t* status, cudaStream_t st);

@@ -1,0 +1,508 @@
+// Product of two arrays of microscaled E2M1 codes, dense or one matrix per expert.
+//
+// D[n][i] = sum_k w[n][k] x[i][k], each value a code times its block's scale:
+// tcgen05.mma kind::mxf4 / kind::mxf4nvf4 multiplies codes and scales exactly and
+// accumulates in fp32 in tensor memory.  The weights are the MMA's A operand (128
+// output channels a CTA, the lanes of tensor memory) and the rows of X its B operand
+// (NT columns), so that one kernel serves a single token (NT = 32) and long batches:
+// with the rows as A, one token would cost the MMAs and operands of 128.
+//
+// Codes arrive by TMA in the 128-byte swizzle, 256 codes a row and K step; scales, 512
+// bytes for 128 rows and four blocks as they lie in memory, go through shared memory
+// into tensor memory by tcgen05.cp, which repeats them for the four groups of lanes.
+// The scales' columns alternate between K steps.
+//
+// Roles: warp 4 copies, one lane of warp 5 issues tcgen05.cp and tcgen05.mma, warps
+// 0-3 and 6-9 take a tile out of tensor memory (32 channels and half of the columns
+// each) while the next tile's MMAs run in the other accumulator.  Every wait is bounded.
+#pragma once
+
+#include "gemm_common.cuh"
+#include "mx_kernels.h"
+
+namespace clq {
+namespace mx {
+
+using gemm::EPI_BYTES;
+using gemm::EPI_COLS;
+
+constexpr int TN = 128;   // output channels a CTA
+constexpr int KC = 256;   // codes of a K step: one 128-byte row
+constexpr int WARP_TMA = 4;
+constexpr int WARP_MMA = 5;
+constexpr int EPI_WARPS = 8;
+constexpr int THREADS = 32 * (EPI_WARPS + 2);
+constexpr int MAX_STAGES = 8;
+
+template <int FMT, int NT, int CG>
+struct Cfg {
+  static constexpr int SC = FMT == CLQ_MX_BLOCK16 ? 4 : 2;  // scale chunks of a K step
+  static constexpr int XB = NT > 128 ? NT / 128 : 1;        // row blocks of X in a tile
+  static constexpr int A = TN * 128;
+  static constexpr int B = NT / CG * 128;
+  static constexpr int SA = SC * 512;
+  static constexpr int SB = XB * SC * 512;
+  static constexpr int STAGE = A + B + SA + SB;
+  static constexpr uint32_t TX = CG * STAGE;
+  static constexpr int PARTS = NT >= 64 ? 2 : 1;  // column shares (four warps each)
+  static constexpr int NCOL = NT / PARTS;
+  static constexpr int FIXED = EPI_WARPS * (EPI_BYTES + NCOL * 4);
+  static constexpr int S0 = (222 * 1024 - FIXED) / STAGE;
+  static constexpr int S = S0 > MAX_STAGES ? MAX_STAGES : S0;
+  static constexpr int OFF_A = 0;
+  static constexpr int OFF_B = OFF_A + S * A;
+  static constexpr int OFF_SA = OFF_B + S * B;
+  static constexpr int OFF_SB = OFF_SA + S * SA;
+  static constexpr int OFF_EPI = OFF_SB + S * SB;
+  static constexpr int OFF_COL = OFF_EPI + EPI_WARPS * EPI_BYTES;
+  static constexpr int BYTES = OFF_COL + EPI_WARPS * NCOL * 4;
+  // Tensor memory: two accumulators of NT columns, two buffers of scales.
+  static constexpr int SFA = 4 * SC;
+  static constexpr int SFB = 4 * SC * XB;
+  static constexpr int SF = SFA + SFB;
+  static constexpr int NEED = 2 * NT + 2 * SF;
+  static constexpr int TMEM = NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
+  // Two accumulators of 256 columns and the scales do not fit: the second then starts
+  // OV columns inside the first, and a tile's MMAs wait for those alone.
+  static constexpr int OV = NEED > 512 ? (NEED - 512 + 31) / 32 * 32 : 0;
+  static constexpr int OFF_SF = 2 * NT - OV;
+  static_assert(OFF_SF + 2 * SF <= TMEM && OV <= NCOL, "tensor memory");
+  static_assert(S >= 3 && STAGE % 1024 == 0, "stages");
+};
+
+struct __align__(8) Bars {
+  uint64_t full[MAX_STAGES];
+  uint64_t empty[MAX_STAGES];
+  uint64_t acc_full[2];
+  uint64_t acc_empty[2];
+  uint64_t ov_empty;  // the overlapped columns have been taken out
+  uint64_t drained;
+  uint32_t tmem_slot;
+  int32_t abort;
+};
+
+// Scales of 32 rows x 16 bytes, shared -> tensor memory, for each group of 32 lanes.
+template <int CG>
+__device__ __forceinline__ void cp_scales(uint32_t taddr, uint64_t desc) {
+  if (CG == 2)
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
+  else
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc)
+                 : "memory");
+}
+
+// Descriptor of 512 contiguous bytes: four 8-row groups of 128 bytes, no swizzle.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem_byte_addr) {
+  return static_cast<uint64_t>((smem_byte_addr >> 4) & 0x3FFFu) |
+         (static_cast<uint64_t>(128u >> 4) << 32) | (static_cast<uint64_t>(1u) << 46);
+}
+
+template <int FMT, int CG>
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                       uint32_t sfa, uint32_t sfb, uint32_t acc) {
+#define CLQ_MX_MMA(G, KIND)                                                              \
+  asm volatile(                                                                          \
+      "{\n\t.reg .pred p;\n\t"                                                           \
+      "setp.ne.b32 p, %4, 0;\n\t"                                                        \
+      "tcgen05.mma.cta_group::" G "." KIND " [%0], %1, %2, %3, [%5], [%6], p;\n\t}" ::   \
+          "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(sfa), "r"(sfb)               \
+      : "memory")
+  if (FMT == CLQ_MX_BLOCK32) {
+    if (CG == 2)
+      CLQ_MX_MMA("2", "kind::mxf4.block_scale.scale_vec::2X");
+    else
+      CLQ_MX_MMA("1", "kind::mxf4.block_scale.scale_vec::2X");
+  } else {
+    if (CG == 2)
+      CLQ_MX_MMA("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else
+      CLQ_MX_MMA("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+  }
+#undef CLQ_MX_MMA
+}
+
+// Instruction descriptor of the block-scaled kinds: E2M1 operands, K-major, K = 64;
+// scale format E8M0 or E4M3; sf: the byte pair of a scale word that the MMA takes.
+__host__ __device__ constexpr uint32_t idesc_mx(int fmt, uint32_t M, uint32_t N, uint32_t sf) {
+  return (sf << 4) | (1u << 7) | (1u << 10) | ((N >> 3) << 17) |
+         ((fmt == CLQ_MX_BLOCK32 ? 1u : 0u) << 23) | ((M >> 4) << 24) | (sf << 29);
+}
+
+__device__ __forceinline__ void stmatrix4_trans(uint32_t addr, const uint32_t (&o)[4]) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr),
+               "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3])
+               : "memory");
+}
+
+// A tile of the output: `n0` its first channel within its matrix, `expert`'s.
+struct Tile {
+  int n0, row0, rows, expert;
+};
+
+template <int NT, int CG, bool GROUPED>
+__device__ __forceinline__ Tile tile_at(const GemmArgs& g, int t, int tiles_n) {
+  const int m = t / tiles_n;
+  Tile r;
+  r.n0 = (t - m * tiles_n) * (TN * CG);
+  if (GROUPED) {
+    const int4 e = __ldg(reinterpret_cast<const int4*>(g.tiles) + m);
+    r.expert = e.x;
+    r.row0 = e.y;
+    r.rows = e.z;
+  } else {
+    r.expert = 0;
+    r.row0 = m * NT;
+    r.rows = min(NT, g.M - r.row0);
+  }
+  return r;
+}
+
+template <typename OutT, int FMT, int NT, int CG, bool GROUPED>
+__global__ void __launch_bounds__(THREADS, 1)
+    mx_gemm_kernel(const __grid_constant__ CUtensorMap mapW,
+                   const __grid_constant__ CUtensorMap mapX,
+                   const __grid_constant__ CUtensorMap mapSW,
+                   const __grid_constant__ CUtensorMap mapSX,
+                   const __grid_constant__ CUtensorMap mapY, GemmArgs g, int use_tma_store) {
+  using C = Cfg<FMT, NT, CG>;
+  constexpr int S = C::S;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ Bars bars;
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(&bars.full[s], 1);
+      mbar_init(&bars.empty[s], 1);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&bars.acc_full[s], 1);
+      mbar_init(&bars.acc_empty[s], CG * 4 * C::PARTS);
+    }
+    mbar_init(&bars.ov_empty, CG * 4);
+    mbar_init(&bars.drained, 1);
+    bars.abort = 0;
+    fence_mbarrier_init();
+  }
+  if (warp == WARP_MMA) {
+    tmem_alloc<CG>(&bars.tmem_slot, C::TMEM);
+  }
+  if (warp == WARP_TMA) {
+    if (elect_one()) {
+      prefetch_tensor_map(&mapW);
+      prefetch_tensor_map(&mapX);
+      prefetch_tensor_map(&mapSW);
+      prefetch_tensor_map(&mapSX);
+      if (use_tma_store) prefetch_tensor_map(&mapY);
+    }
+  }
+  __syncwarp();  // the cluster barrier counts whole warps: none may come to it in parts
+  tc_fence_before();
+  if (CG == 2)
+    cluster_sync();
+  else
+    __syncthreads();
+  tc_fence_after();
+  // The permit to allocate belongs to the pair: given up by one CTA while the other's
+  // allocation is still on its way, it leaves that allocation waiting for ever (seen once
+  // in 10^4 to 10^5 launches), so both have allocated first.
+  if (warp == WARP_MMA) tmem_relinquish<CG>();
+  const uint32_t tmem = bars.tmem_slot;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  volatile int32_t* abort = &bars.abort;
+  const int nk = (g.K + KC - 1) / KC;
+  const int tiles_n = (g.N + TN * CG - 1) / (TN * CG);
+  const int tiles = (GROUPED ? __ldg(g.tile_count) : (g.M + NT - 1) / NT) * tiles_n;
+  const int unit = static_cast<int>(blockIdx.x) / CG;
+  const int units = static_cast<int>(gridDim.x) / CG;
+  const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
+
+  if (warp == WARP_TMA) {
+    if (elect_one()) {
+      int it = 0, s = 0;
+      uint32_t phase = 1;
+      bool ok = true;
+      const uint32_t full0 = CG == 2 ? cluster_addr(&bars.full[0], 0) : 0;
+      for (int t = unit; t < tiles && ok; t += units) {
+        const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
+        const int n0 = T.n0 + rank * TN;
+        const int wrow = T.expert * g.N + n0;
+        const int xrow = T.row0 + rank * (NT / CG);
+        const int wchunk = (T.expert * g.w_blocks + n0 / kRowBlock) * g.chunks;
+        const int xchunk = T.row0 / kRowBlock * g.chunks;
+        for (int kb = 0; kb < nk; ++kb, ++it) {
+          if (!mbar_wait_bounded(&bars.empty[s], phase, abort, g.status, kWaitLimitNs)) {
+            ok = false;
+            break;
+          }
+          uint64_t* full = &bars.full[s];
+          if (CG == 1 || rank == 0) mbar_arrive_expect_tx(full, C::TX);
+          auto load = [&](int off, const CUtensorMap* map, int x, int y) {
+            if constexpr (CG == 2)
+              tma_load_2d_pair(smem + off, map, x, y, full0 + 8u * s);
+            else
+              tma_load_2d(smem + off, map, x, y, full);
+          };
+          load(C::OFF_A + s * C::A, &mapW, kb * 128, wrow);
+          load(C::OFF_B + s * C::B, &mapX, kb * 128, xrow);
+          load(C::OFF_SA + s * C::SA, &mapSW, 0, wchunk + kb * C::SC);
+#pragma unroll
+          for (int j = 0; j < C::XB; ++j)
+            load(C::OFF_SB + s * C::SB + j * C::SC * 512, &mapSX, 0,
+                 xchunk + j * g.chunks + kb * C::SC);
+          if (++s == S) {
+            s = 0;
+            phase ^= 1;
+          }
+        }
+      }
+      // On an abort the copies in flight land before exit (a pair's second CTA, whose
+      // copies complete on the leader's barriers, allows them a millisecond).
+      if (!ok && rank != 0) {
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 1000000ull) __nanosleep(1000);
+      } else if (!ok) {
+        for (int j = max(0, it - S); j < it; ++j)
+          mbar_wait_bounded(&bars.full[j % S], (j / S) & 1, nullptr, nullptr, 10000000ull);
+      }
+    }
+    __syncwarp();
+  } else if (warp == WARP_MMA) {
+    if (rank == 0 && elect_one()) {
+      const uint64_t adesc = sw128_desc(smem_addr(smem + C::OFF_A));
+      const uint64_t bdesc = sw128_desc(smem_addr(smem + C::OFF_B));
+      const uint64_t sadesc = scale_desc(smem_addr(smem + C::OFF_SA));
+      const uint64_t sbdesc = scale_desc(smem_addr(smem + C::OFF_SB));
+      int s = 0, tc = 0;
+      uint32_t phase = 0, sfbuf = 0;
+      bool ok = true;
+      for (int t = unit; t < tiles && ok; t += units, ++tc) {
+        const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
+        // a 64-row tile may be the second half of its scale block
+        const uint32_t xcol = NT == 64 ? static_cast<uint32_t>(T.row0 & 64) / 32u : 0u;
+        const int buf = tc & 1;
+        if (!mbar_wait_bounded(&bars.acc_empty[buf], ((tc >> 1) & 1) ^ 1, abort, g.status,
+                               kWaitLimitNs) ||
+            (C::OV > 0 && tc > 0 &&
+             !mbar_wait_bounded(&bars.ov_empty, (tc - 1) & 1, abort, g.status, kWaitLimitNs))) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t d = tmem + buf * (NT - C::OV);
+        for (int kb = 0; kb < nk; ++kb) {
+          if (!mbar_wait_bounded(&bars.full[s], phase, abort, g.status, kWaitLimitNs)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint32_t sfa = tmem + C::OFF_SF + sfbuf * C::SF;
+          const uint32_t sfb = sfa + C::SFA;
+#pragma unroll
+          for (int c = 0; c < C::SC; ++c) {
+            cp_scales<CG>(sfa + 4 * c, sadesc + static_cast<uint32_t>((s * C::SA + c * 512) / 16));
+#pragma unroll
+            for (int j = 0; j < C::XB; ++j)
+              cp_scales<CG>(sfb + 4 * (c * C::XB + j),
+                            sbdesc + static_cast<uint32_t>((s * C::SB + (j * C::SC + c) * 512) / 16));
+          }
+          const uint64_t a0 = adesc + static_cast<uint32_t>(s * (C::A / 16));
+          const uint64_t b0 = bdesc + static_cast<uint32_t>(s * (C::B / 16));
+          // MMAs of 64 codes; past the end of a row there are codes of zero, but no scales
+          const int steps = min(KC / 64, (g.K - kb * KC + 63) / 64);
+#pragma unroll
+          for (int k = 0; k < KC / 64; ++k) {
+            if (k < steps) {
+              const int c = FMT == CLQ_MX_BLOCK32 ? k >> 1 : k;
+              const uint32_t sf = FMT == CLQ_MX_BLOCK32 ? (k & 1) * 2 : 0;
+              mma_mx<FMT, CG>(d, a0 + k * 2, b0 + k * 2, idesc_mx(FMT, TN * CG, NT, sf),
+                              sfa + 4 * c, sfb + 4 * C::XB * c + xcol, (kb | k) == 0 ? 0u : 1u);
+            }
+          }
+          mma_commit<CG>(&bars.empty[s]);
+          sfbuf ^= 1;
+          if (++s == S) {
+            s = 0;
+            phase ^= 1;
+          }
+        }
+        if (ok) mma_commit<CG>(&bars.acc_full[buf]);
+      }
+      mma_commit<CG>(&bars.drained);
+      mbar_wait_bounded(&bars.drained, 0, nullptr, nullptr, 10000000ull);
+    } else if (CG == 2 && rank == 1 && elect_one()) {
+      // The leader's commits signal this CTA's barriers too: it stays for the last one.
+      mbar_wait_bounded(&bars.drained, 0, abort, nullptr, 2 * kWaitLimitNs);
+    }
+    __syncwarp();
+  } else if (warp < 4 || C::PARTS == 2) {
+    const int quarter = warp & 3;
+    const int part = warp < 4 ? 0 : 1;
+    const int ew = part * 4 + quarter;
+    uint8_t* staging = smem + C::OFF_EPI + ew * EPI_BYTES;
+    const uint32_t stage_addr = smem_addr(staging);
+    float* col = reinterpret_cast<float*>(smem + C::OFF_COL) + ew * C::NCOL;
+    const uint32_t empty0 = CG == 2 ? cluster_addr(&bars.acc_empty[0], 0) : 0;
+    const uint32_t ov0 = CG == 2 ? cluster_addr(&bars.ov_empty, 0) : 0;
+    constexpr int NB = C::NCOL / EPI_COLS;  // blocks of 32 rows of X
+    int tc = 0;
+    for (int t = unit; t < tiles; t += units, ++tc) {
+      const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
+      const int n0 = T.n0 + rank * TN + quarter * 32;  // this warp's channels
+      const int col0 = part * C::NCOL;                 // and tile columns
+      const int buf = tc & 1;
+      // channels 8 k + lane / 4 of a thread's fragments; row scales of the warp's columns
+      float sw[4], bi[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = n0 + 8 * k + (lane >> 2);
+        const bool in = n < g.N;
+        const size_t at = static_cast<size_t>(T.expert) * g.N + n;
+        sw[k] = g.inv_b;
+        if (FMT == CLQ_MX_BLOCK16) sw[k] = in ? __ldg(g.s_w + at) * g.inv_b : 0.f;
+        bi[k] = in && g.bias != nullptr
+                    ? Num<OutT>::to_f(__ldg(static_cast<const uint16_t*>(g.bias) + at))
+                    : 0.f;
+      }
+      if (FMT == CLQ_MX_BLOCK16) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const int i = col0 + 32 * j + lane;
+          col[32 * j + lane] = i < T.rows ? __ldg(g.s_x + T.row0 + i) : 0.f;
+        }
+        __syncwarp();
+      }
+      bool ok = mbar_wait_bounded(&bars.acc_full[buf], (tc >> 1) & 1, abort, g.status,
+                                  kWaitLimitNs);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      auto arrive = [&](uint64_t* bar, uint32_t remote) {
+        tc_fence_before();
+        __syncwarp();
+        if (elect_one()) {
+          if (CG == 2)
+            mbar_arrive_cluster(remote);
+          else
+            mbar_arrive(bar);
+        }
+      };
+      // The columns that the other accumulator overlaps are the first ones of the second
+      // accumulator and the last ones of the first: they are taken out first.
+      const bool down = C::OV > 0 && buf == 0;
+      const bool guards = C::OV > 0 && part == (buf == 0 ? 1 : 0);
+      const uint32_t lane_base =
+          tmem + buf * (NT - C::OV) + (static_cast<uint32_t>(quarter * 32) << 16);
+      const int live = n0 < g.N ? max(0, min(NB, (T.rows - col0 + 31) / 32)) : 0;
+#pragma unroll 1
+      for (int j = 0; j < NB; ++j) {
+        const int blk = down ? NB - 1 - j : j;
+        if (blk < live) {
+          const int c = col0 + blk * EPI_COLS;
+          uint32_t r[2][16];  // channels 0 .. 15 and 16 .. 31
+          gemm::tmem_ld_frag(lane_base + c, r[0]);
+          gemm::tmem_ld_frag(lane_base + (16u << 16) + c, r[1]);
+          float2 sx[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            sx[q] = FMT == CLQ_MX_BLOCK16 ? *reinterpret_cast<const float2*>(
+                                                col + blk * 32 + 8 * q + 2 * (lane & 3))
+                                          : make_float2(1.f, 1.f);
+          gemm::tmem_ld_wait_tie(r[0]);
+          gemm::tmem_ld_wait_tie(r[1]);
+          if (use_tma_store && elect_one()) gemm::bulk_wait_read<0>();
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {  // rows 8 q + 2 (lane % 4), + 1
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float2 acc = make_float2(__uint_as_float(r[k >> 1][4 * q + 2 * (k & 1)]),
+                                             __uint_as_float(r[k >> 1][4 * q + 2 * (k & 1) + 1]));
+              const float2 s2 = __fmul2_rn(make_float2(sw[k], sw[k]), sx[q]);
+              const float2 v = __ffma2_rn(acc, s2, make_float2(bi[k], bi[k]));
+              o[k] = Num<OutT>::pack2(v.x, v.y);
+            }
+            stmatrix4_trans(stage_addr + gemm::staged_chunk(8 * q + (lane & 7), lane >> 3), o);
+          }
+          if (use_tma_store) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (elect_one()) {
+              gemm::tma_store_2d(&mapY, staging, n0, T.row0 + c);
+              gemm::bulk_commit();
+            }
+          } else {
+            __syncwarp();
+            gemm::store_block_direct(stage_addr, lane, T.row0 + c, T.row0 + T.rows, n0, g.N,
+                                     static_cast<uint16_t*>(g.Y));
+            __syncwarp();
+          }
+        }
+        if (C::OV > 0 && guards && j == C::OV / 32 - 1) arrive(&bars.ov_empty, ov0);
+      }
+      arrive(&bars.acc_empty[buf], empty0 + 8u * buf);
+    }
+    if (elect_one()) gemm::bulk_wait_all();
+    __syncwarp();
+  }
+  tc_fence_before();
+  if (CG == 2)
+    cluster_sync();
+  else
+    __syncthreads();
+  if (warp == WARP_MMA) {
+    tc_fence_after();
+    tmem_dealloc<CG>(tmem, C::TMEM);
+  }
+  if (CG == 2) {  // nor does a CTA of a pair leave before the other has deallocated
+    __syncwarp();
+    cluster_sync();
+  }
+}
+
+struct GemmMaps {
+  CUtensorMap W, X, SW, SX, Y;
+};
+
+template <typename OutT, int FMT, int NT, int CG, bool GROUPED>
+cudaError_t launch_gemm_t(const GemmMaps& m, const GemmArgs& g, int use_tma_store, int grid,
+                          cudaStream_t st) {
+  using C = Cfg<FMT, NT, CG>;
+  auto k = mx_gemm_kernel<OutT, FMT, NT, CG, GROUPED>;
+  constexpr size_t smem = C::BYTES + 1024;
+  cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, THREADS, nullptr);
+  if (e != cudaSuccess) return e;
+  return launch_cluster_pdl(k, grid, CG, THREADS, smem, st, m.W, m.X, m.SW, m.SX, m.Y, g,
+                            use_tma_store);
+}
+
+// The tile of nt rows (cg CTAs): instantiated for each output type and format in
+// mx_gemm_*.cu.
+template <typename OutT, int FMT>
+cudaError_t launch_gemm_tiles(const GemmMaps& m, const GemmArgs& g, int nt, bool grouped,
+                              int use_tma_store, int grid, cudaStream_t st) {
+#define CLQ_MX_GO(NT, CG)                                                               \
+  return grouped ? launch_gemm_t<OutT, FMT, NT, CG, true>(m, g, use_tma_store, grid, st) \
+                 : launch_gemm_t<OutT, FMT, NT, CG, false>(m, g, use_tma_store, grid, st)
+  switch (nt) {
+    case 32: CLQ_MX_GO(32, 1);
+    case 128: CLQ_MX_GO(128, 1);
+    default: CLQ_MX_GO(256, 2);
+  }
+#undef CLQ_MX_GO
+}
+
+using GemmFn = cudaError_t (*)(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+cudaError_t gemm_block32_f16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+cudaError_t gemm_block32_bf16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+cudaError_t gemm_block16_f16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+cudaError_t gemm_block16_bf16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+
+}  // namespace mx
+}  // namespace clq

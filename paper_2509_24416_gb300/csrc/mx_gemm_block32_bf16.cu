@@ -1,0 +1,11 @@
+// Microscaled product, blocks of 32, bf16 outputs.
+#include "mx_gemm.cuh"
+
+namespace clq {
+namespace mx {
+cudaError_t gemm_block32_bf16(const GemmMaps& m, const GemmArgs& g, int nt, bool grouped,
+                            int use_tma_store, int grid, cudaStream_t st) {
+  return launch_gemm_tiles<__nv_bfloat16, CLQ_MX_BLOCK32>(m, g, nt, grouped, use_tma_store, grid, st);
+}
+}  // namespace mx
+}  // namespace clq

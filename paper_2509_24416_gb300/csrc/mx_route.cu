@@ -1,0 +1,441 @@
+// Routing of tokens to experts, the rows that a routing gives them, and the weighted
+// sum of what comes back.
+#include "clq_device.cuh"
+#include "mx_kernels.h"
+
+#include <cfloat>
+
+namespace clq {
+namespace mx {
+namespace {
+
+constexpr uint32_t kAll = 0xffffffffu;
+constexpr int ROUTE_WARPS = 8;
+
+// Order-preserving bits of a float (no NaN); -0 as +0.
+__device__ __forceinline__ uint32_t ordered(float f) {
+  const uint32_t u = __float_as_uint(__fadd_rn(f, 0.f));
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+constexpr uint32_t kMasked = 0x007FFFFFu;  // ordered(-infinity)
+
+template <typename T>
+__device__ __forceinline__ float load_logit(const void* p, size_t i) {
+  return Num<T>::to_f(__ldg(static_cast<const uint16_t*>(p) + i));
+}
+template <>
+__device__ __forceinline__ float load_logit<float>(const void* p, size_t i) {
+  return __ldg(static_cast<const float*>(p) + i);
+}
+
+// Largest key of the warp and the lowest expert that has it; key[i] belongs to expert
+// 32 i + lane.
+template <int C>
+__device__ __forceinline__ uint32_t warp_best(const uint32_t (&key)[C], int lane, int* at) {
+  uint32_t m = key[0];
+#pragma unroll
+  for (int i = 1; i < C; ++i) m = max(m, key[i]);
+  const uint32_t best = __reduce_max_sync(kAll, m);
+  uint32_t e = 0x7FFFFFFFu;
+#pragma unroll
+  for (int i = C - 1; i >= 0; --i)
+    if (key[i] == best) e = 32 * i + lane;
+  *at = static_cast<int>(__reduce_min_sync(kAll, e));
+  return best;
+}
+
+// One warp a token, 32 C >= E.  The largest is taken k times: keys in registers, one
+// reduction over the warp for the value and one for the lowest index that has it.
+template <typename T, int C>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int t = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_launch_dependents();
+  if (t >= a.T) return;
+  float p[C];
+  uint32_t key[C];
+  bool masked[C];
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int e = 32 * i + lane;
+    const float x = e < a.E ? load_logit<T>(a.logits, static_cast<size_t>(t) * a.ld + e) : -INFINITY;
+    masked[i] = x == -INFINITY || x != x;
+    p[i] = fminf(x, FLT_MAX);
+    if (!masked[i]) most = fmaxf(most, p[i]);
+  }
+  if (a.scoring == 0) {
+    // (a float's order is that of its ordered bits)
+    most = unordered(__reduce_max_sync(kAll, ordered(most)));
+    float s[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      p[i] = masked[i] ? 0.f : expf(__fsub_rn(p[i], most));
+      s[i] = p[i];
+    }
+    // by halves: C is a power of two, and halves beyond E add zeros
+#pragma unroll
+    for (int h = C / 2; h >= 1; h /= 2)
+#pragma unroll
+      for (int i = 0; i < h; ++i) s[i] = __fadd_rn(s[i], s[i + h]);
+#pragma unroll
+    for (int h = 16; h >= 1; h /= 2) s[0] = __fadd_rn(s[0], __shfl_xor_sync(kAll, s[0], h));
+#pragma unroll
+    for (int i = 0; i < C; ++i) p[i] = __fdiv_rn(p[i], s[0]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < C; ++i) p[i] = __fdiv_rn(1.f, __fadd_rn(1.f, expf(-p[i])));
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int e = 32 * i + lane;
+    float c = p[i];
+    if (a.balance != nullptr && e < a.E) c = __fadd_rn(c, __ldg(a.balance + e));
+    key[i] = masked[i] || c != c ? kMasked : ordered(c);
+  }
+  if (a.groups > 1) {
+    const int size = a.E / a.groups;
+    uint32_t gkey = 0;  // lane g: group g (at most 32)
+    for (int g = 0; g < a.groups; ++g) {
+      uint32_t in[C];
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        const int e = 32 * i + lane;
+        in[i] = e >= g * size && e < (g + 1) * size ? key[i] : 0u;
+      }
+      int at;
+      const uint32_t first = warp_best<C>(in, lane, &at);
+      float sum = unordered(first);
+      if (a.group_top == 2 && size > 1) {
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+          if (32 * i + lane == at) in[i] = 0u;
+        sum = __fadd_rn(sum, unordered(warp_best<C>(in, lane, &at)));
+      }
+      if (lane == g) gkey = ordered(sum);
+    }
+    uint32_t keep = 0;
+    for (int j = 0; j < a.top_groups; ++j) {
+      const uint32_t best = __reduce_max_sync(kAll, gkey);
+      const int g = __ffs(__ballot_sync(kAll, gkey == best)) - 1;
+      keep |= 1u << g;
+      if (lane == g) gkey = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const int e = 32 * i + lane;
+      if (e < a.E && !((keep >> (e / size)) & 1u)) key[i] = kMasked;
+    }
+  }
+  // lane j keeps the j-th choice
+  int mine = -1;
+  float w = 0.f, total = 0.f;
+  for (int j = 0; j < a.k; ++j) {
+    int at;
+    const uint32_t best = warp_best<C>(key, lane, &at);
+    if (best <= kMasked) break;  // nothing left but masked experts
+    float v = 0.f;
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (32 * i + lane == at) {
+        key[i] = 0u;
+        v = p[i];
+      }
+    v = __shfl_sync(kAll, v, at & 31);
+    total += v;
+    if (lane == j) {
+      mine = at;
+      w = v;
+    }
+  }
+  if (a.renormalize) w = total > 0.f ? __fdiv_rn(w, total) : 0.f;
+  if (lane < a.k) {
+    a.experts[static_cast<size_t>(t) * a.k + lane] = mine;
+    a.weights[static_cast<size_t>(t) * a.k + lane] = w * a.scale;
+  }
+}
+
+// ------------------------------------------------------------------- plan ---
+constexpr int CHUNK = 32;  // tokens a bit mask holds
+constexpr int PLAN_THREADS = 512;
+
+// Rows of experts e = threadIdx.x .. < E with counts[e] rows each: where each starts,
+// and the tiles that cover them.  One block; E <= blockDim.x.
+__device__ void plan_tiles(int count, int E, int32_t* start, int32_t* counts, RowTile* t128,
+                           RowTile* t256) {
+  __shared__ int32_t sum[3][PLAN_THREADS / 32];
+  const int e = threadIdx.x, lane = e & 31, warp = e >> 5;
+  const int n128 = (count + 127) / 128, n256 = (count + 255) / 256;
+  int a = n128, b = n256;  // inclusive sums over the experts
+  for (int o = 1; o < 32; o *= 2) {
+    const int x = __shfl_up_sync(kAll, a, o), y = __shfl_up_sync(kAll, b, o);
+    if (lane >= o) {
+      a += x;
+      b += y;
+    }
+  }
+  if (lane == 31) {
+    sum[0][warp] = a;
+    sum[1][warp] = b;
+  }
+  __syncthreads();
+  for (int w = 0; w < warp; ++w) {
+    a += sum[0][w];
+    b += sum[1][w];
+  }
+  if (e < E) {
+    const int at = a - n128;
+    start[e] = at * kRowBlock;
+    for (int i = 0; i < n128; ++i)
+      t128[at + i] = RowTile{e, (at + i) * kRowBlock, min(128, count - 128 * i), 0};
+    for (int i = 0; i < n256; ++i)
+      t256[b - n256 + i] = RowTile{e, (at + 2 * i) * kRowBlock, min(256, count - 256 * i), 0};
+    if (e == E - 1) {
+      counts[0] = a;
+      counts[1] = b;
+    }
+  }
+}
+
+// Chunk c: hist[e][c] = tokens of the chunk that name expert e.
+__global__ void __launch_bounds__(256) plan_hist_kernel(const int32_t* __restrict__ experts, int T,
+                                                        int k, int E, int chunks,
+                                                        uint8_t* __restrict__ hist) {
+  extern __shared__ uint32_t mask[];  // [E]
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int e = threadIdx.x; e < E; e += blockDim.x) mask[e] = 0;
+  __syncthreads();
+  const int t0 = blockIdx.x * CHUNK;
+  const int n = min(CHUNK, T - t0) * k;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int e = __ldg(experts + static_cast<size_t>(t0) * k + i);
+    if (e >= 0 && e < E) atomicOr(&mask[e], 1u << (i / k));
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < E; e += blockDim.x)
+    hist[static_cast<size_t>(e) * chunks + blockIdx.x] = static_cast<uint8_t>(__popc(mask[e]));
+}
+
+// One warp an expert: prefix[e][c] = rows of e in the chunks before c, count[e].
+__global__ void plan_prefix_kernel(const uint8_t* __restrict__ hist, int E, int chunks,
+                                   int32_t* __restrict__ prefix, int32_t* __restrict__ count) {
+  const int e = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (e >= E) return;
+  int carry = 0;
+  for (int c0 = 0; c0 < chunks; c0 += 32) {
+    const int c = c0 + lane;
+    const int n = c < chunks ? hist[static_cast<size_t>(e) * chunks + c] : 0;
+    int s = n;
+    for (int o = 1; o < 32; o *= 2) {
+      const int x = __shfl_up_sync(kAll, s, o);
+      if (lane >= o) s += x;
+    }
+    if (c < chunks) prefix[static_cast<size_t>(e) * chunks + c] = carry + s - n;
+    carry += __shfl_sync(kAll, s, 31);
+  }
+  if (lane == 0) count[e] = carry;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS)
+    plan_start_kernel(const int32_t* __restrict__ count, int E, int32_t* start, int32_t* counts,
+                      RowTile* t128, RowTile* t256) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int n = static_cast<int>(threadIdx.x) < E ? count[threadIdx.x] : 0;
+  plan_tiles(n, E, start, counts, t128, t256);
+}
+
+__global__ void __launch_bounds__(256)
+    plan_rows_kernel(const int32_t* __restrict__ experts, int T, int k, int E, int chunks,
+                     const int32_t* __restrict__ prefix, const int32_t* __restrict__ start,
+                     int32_t* __restrict__ rows) {
+  extern __shared__ uint32_t mask[];  // [E]
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int e = threadIdx.x; e < E; e += blockDim.x) mask[e] = 0;
+  __syncthreads();
+  const int t0 = blockIdx.x * CHUNK;
+  const int n = min(CHUNK, T - t0) * k;
+  const size_t at = static_cast<size_t>(t0) * k;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int e = __ldg(experts + at + i);
+    if (e >= 0 && e < E) atomicOr(&mask[e], 1u << (i / k));
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int e = __ldg(experts + at + i);
+    int r = -1;
+    if (e >= 0 && e < E)
+      r = start[e] + prefix[static_cast<size_t>(e) * chunks + blockIdx.x] +
+          __popc(mask[e] & ((1u << (i / k)) - 1u));
+    rows[at + i] = r;
+  }
+}
+
+// All of it in one block, for up to SMALL_CHUNKS chunks of tokens: masks [chunks][E].
+constexpr int SMALL_CHUNKS = 16;
+__global__ void __launch_bounds__(PLAN_THREADS)
+    plan_small_kernel(const int32_t* __restrict__ experts, int T, int k, int E, int chunks,
+                      int32_t* start, int32_t* counts, RowTile* t128, RowTile* t256,
+                      int32_t* __restrict__ rows) {
+  extern __shared__ uint32_t mask[];  // [chunks][E]; then first[E], starts
+  __shared__ int32_t first[PLAN_THREADS];
+  pdl_wait();
+  pdl_launch_dependents();
+  for (int i = threadIdx.x; i < chunks * E; i += blockDim.x) mask[i] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < T * k; i += blockDim.x) {
+    const int e = __ldg(experts + i), t = i / k;
+    if (e >= 0 && e < E) atomicOr(&mask[(t / CHUNK) * E + e], 1u << (t % CHUNK));
+  }
+  __syncthreads();
+  int n = 0;
+  if (static_cast<int>(threadIdx.x) < E)
+    for (int c = 0; c < chunks; ++c) n += __popc(mask[c * E + threadIdx.x]);
+  plan_tiles(n, E, first, counts, t128, t256);
+  __syncthreads();
+  for (int i = threadIdx.x; i < T * k; i += blockDim.x) {
+    const int e = __ldg(experts + i), t = i / k;
+    int r = -1;
+    if (e >= 0 && e < E) {
+      r = first[e] + __popc(mask[(t / CHUNK) * E + e] & ((1u << (t % CHUNK)) - 1u));
+      for (int c = 0; c < t / CHUNK; ++c) r += __popc(mask[c * E + e]);
+    }
+    rows[i] = r;
+  }
+}
+
+// ---------------------------------------------------------------- combine ---
+// One thread eight columns of a token.
+template <typename T>
+__global__ void __launch_bounds__(256)
+    combine_kernel(const uint4* __restrict__ Y, const int32_t* __restrict__ rows,
+                   const float* __restrict__ weights, int tokens, int k, int D, int R, uint4* out,
+                   int32_t* status) {
+  const int units = D / 8;
+  const size_t n = static_cast<size_t>(tokens) * units;
+  pdl_wait();
+  pdl_launch_dependents();
+  for (size_t i = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x; i < n;
+       i += static_cast<size_t>(gridDim.x) * blockDim.x) {
+    const size_t t = i / units;
+    const int u = static_cast<int>(i - t * units);
+    float s[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = 0.f;
+    for (int j = 0; j < k; ++j) {
+      const int r = __ldg(rows + t * k + j);
+      if (r < 0) continue;
+      if (r >= R) {
+        record_status(status, CLQ_ERR_DEVICE_INDEX);
+        continue;
+      }
+      const float w = __ldg(weights + t * k + j);
+      const uint4 p = __ldg(Y + static_cast<size_t>(r) * units + u);
+      const uint32_t q[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        s[2 * h] = fmaf(w, Num<T>::to_f(static_cast<uint16_t>(q[h])), s[2 * h]);
+        s[2 * h + 1] = fmaf(w, Num<T>::to_f(static_cast<uint16_t>(q[h] >> 16)), s[2 * h + 1]);
+      }
+    }
+    out[i] = make_uint4(Num<T>::pack2(s[0], s[1]), Num<T>::pack2(s[2], s[3]),
+                        Num<T>::pack2(s[4], s[5]), Num<T>::pack2(s[6], s[7]));
+  }
+}
+
+template <typename T>
+cudaError_t route_t(const RouteArgs& a, cudaStream_t st) {
+  const int grid = (a.T + ROUTE_WARPS - 1) / ROUTE_WARPS;
+  const int threads = 32 * ROUTE_WARPS;
+  if (a.E <= 32) return launch_pdl(route_kernel<T, 1>, grid, threads, 0, st, a);
+  if (a.E <= 64) return launch_pdl(route_kernel<T, 2>, grid, threads, 0, st, a);
+  if (a.E <= 128) return launch_pdl(route_kernel<T, 4>, grid, threads, 0, st, a);
+  if (a.E <= 256) return launch_pdl(route_kernel<T, 8>, grid, threads, 0, st, a);
+  return launch_pdl(route_kernel<T, 16>, grid, threads, 0, st, a);
+}
+
+}  // namespace
+
+PlanLayout plan_layout(int T, int k, int E) {
+  PlanLayout p{};
+  const int64_t n = static_cast<int64_t>(T) * k;
+  const int64_t used = std::min<int64_t>(E, n);
+  p.chunks = (T + CHUNK - 1) / CHUNK;
+  p.max128 = plan_rows(T, k, E) / kRowBlock;
+  p.max256 = static_cast<int>((n + 255 * used) / 256);
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = (off + bytes + 255) & ~static_cast<size_t>(255);
+    return at;
+  };
+  p.counts_off = take(16);
+  p.tiles128_off = take(static_cast<size_t>(p.max128) * sizeof(RowTile));
+  p.tiles256_off = take(static_cast<size_t>(p.max256) * sizeof(RowTile));
+  p.start_off = take(static_cast<size_t>(2 * E) * 4);  // starts, then row counts
+  if (p.chunks > SMALL_CHUNKS) {
+    p.hist_off = take(static_cast<size_t>(E) * p.chunks);
+    p.prefix_off = take(static_cast<size_t>(E) * p.chunks * 4);
+  }
+  p.bytes = off;
+  return p;
+}
+
+cudaError_t launch_route(const RouteArgs& a, int dtype, cudaStream_t st) {
+  return dtype == CLQ_F32   ? route_t<float>(a, st)
+         : dtype == CLQ_F16 ? route_t<__half>(a, st)
+                            : route_t<__nv_bfloat16>(a, st);
+}
+
+cudaError_t launch_plan(const int32_t* experts, int T, int k, int E, int32_t* out_rows, void* plan,
+                        const PlanLayout& pl, cudaStream_t st) {
+  uint8_t* p = static_cast<uint8_t*>(plan);
+  int32_t* counts = reinterpret_cast<int32_t*>(p + pl.counts_off);
+  int32_t* start = reinterpret_cast<int32_t*>(p + pl.start_off);
+  RowTile* t128 = reinterpret_cast<RowTile*>(p + pl.tiles128_off);
+  RowTile* t256 = reinterpret_cast<RowTile*>(p + pl.tiles256_off);
+  if (pl.chunks <= SMALL_CHUNKS)  // at most 16 * 512 masks of 4 bytes: 32 KB
+    return launch_pdl(plan_small_kernel, 1, PLAN_THREADS,
+                      static_cast<size_t>(pl.chunks) * E * 4, st, experts, T, k, E, pl.chunks,
+                      start, counts, t128, t256, out_rows);
+  uint8_t* hist = p + pl.hist_off;
+  int32_t* prefix = reinterpret_cast<int32_t*>(p + pl.prefix_off);
+  const size_t smem = static_cast<size_t>(E) * 4;
+  cudaError_t e = launch_pdl(plan_hist_kernel, pl.chunks, 256, smem, st, experts, T, k, E,
+                             pl.chunks, hist);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(plan_prefix_kernel, (E + 7) / 8, 256, 0, st, const_cast<const uint8_t*>(hist), E,
+                 pl.chunks, prefix, start + E);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(plan_start_kernel, 1, PLAN_THREADS, 0, st, const_cast<const int32_t*>(start + E),
+                 E, start, counts, t128, t256);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(plan_rows_kernel, pl.chunks, 256, smem, st, experts, T, k, E, pl.chunks,
+                    const_cast<const int32_t*>(prefix), const_cast<const int32_t*>(start),
+                    out_rows);
+}
+
+cudaError_t launch_combine(const void* Y, int dtype, const int32_t* rows, const float* weights,
+                           int T, int k, int D, int R, void* out, int32_t* status,
+                           cudaStream_t st) {
+  const int sms = sm_count();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  const size_t n = static_cast<size_t>(T) * (D / 8);
+  const int grid = static_cast<int>(std::min<size_t>((n + 255) / 256, 8u * sms));
+  auto k16 = combine_kernel<__half>;
+  auto kb = combine_kernel<__nv_bfloat16>;
+  return launch_pdl(dtype == CLQ_F16 ? k16 : kb, grid, 256, 0, st, static_cast<const uint4*>(Y),
+                    rows, weights, T, k, D, R, static_cast<uint4*>(out), status);
+}
+
+}  // namespace mx
+}  // namespace clq

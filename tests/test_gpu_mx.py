@@ -1,0 +1,350 @@
+"""Microscaled operators on the GPU against their definitions in 64 bits (mx_utils)."""
+import numpy as np
+import pytest
+import torch
+
+import mx_utils as ref
+from paper_2509_24416_gb300 import clq, mx
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+DEV = "cuda"
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def rows_of(g, M, K, dtype):
+    """N(0, 1) with a few large channels."""
+    s = torch.ones(K, device=DEV)
+    s[torch.randperm(K, generator=g, device=DEV)[:max(1, K // 50)]] = 37.0
+    return (torch.randn((M, K), generator=g, device=DEV) * s).to(dtype)
+
+
+def perm_of(g, K):
+    return torch.randperm(K, generator=g, device=DEV).to(torch.int32)
+
+
+def to64(t):
+    return t.detach().cpu().double().numpy()
+
+
+@pytest.fixture(autouse=True)
+def no_device_error():
+    yield
+    assert clq.device_status() == 0
+
+
+def check_quantized(q, v, slack=0.0):
+    """q holds the codes of v (float64, [rows, K]); slack: relative error of the library's v."""
+    fmt, block = q.fmt, ref.BLOCK[q.fmt]
+    w = v.reshape(v.shape[0], -1, block)
+    amax = np.abs(w).max(2)
+    byte = ref.scale_bytes(q.scales, q.rows, q.K // block)
+    if fmt == "block32":
+        with np.errstate(divide="ignore"):
+            e = np.maximum(np.ceil(np.log2(amax / 6)), -127)
+        if slack == 0:
+            np.testing.assert_array_equal(byte, e + 127)
+        else:
+            near = np.abs(np.log2(np.maximum(amax, 1e-300) / 6) - np.rint(np.log2(np.maximum(amax, 1e-300) / 6))) < 4 * slack
+            assert np.all((byte == e + 127) | near)
+    else:
+        row = q.row_scale.cpu().numpy().astype(np.float64)
+        np.testing.assert_allclose(row, np.maximum(amax.max(1) / 2688, 2.0 ** -100), rtol=2.0 ** -23 + slack)
+        t = amax / (6 * row[:, None])
+        step = np.where(t < 2.0 ** -6, 2.0 ** -9, 2.0 ** (np.floor(np.log2(np.maximum(t, 2.0 ** -6))) - 3))
+        # nearest E4M3 value, up to the fp32 steps' error
+        assert np.all(np.abs(ref.e4m3(byte) - np.minimum(t, 448)) <= step * 0.5 + t * (2.0 ** -21 + 2 * slack))
+    s = ref.scales_of(q)
+    x = np.where(s[:, :, None] > 0, w / np.where(s > 0, s, 1)[:, :, None], 0)
+    code = ref.codes_of(q.codes).reshape(w.shape)
+    miss = ref.nearest_slack(x, code)
+    assert miss.max() <= (0 if fmt == "block32" and slack == 0 else 6 * 2.0 ** -21 + 12 * slack)
+
+
+SHAPES = [(1, 32), (3, 64), (33, 96), (127, 160), (128, 1152), (129, 1184), (5, 4608), (2, 16384), (300, 256)]
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K", SHAPES)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_quantize(fmt, M, K, dtype):
+    X = rows_of(gen(M * K), M, K, dtype)
+    q = mx.quantize(X, fmt)
+    check_quantized(q, to64(X))
+    for out in (F16, BF16):
+        got, want = to64(mx.dequantize(q, out)), ref.values_of(q)
+        eps = 2.0 ** -11 if out == F16 else 2.0 ** -8
+        assert np.all(np.abs(got - want) <= np.abs(want) * eps * 1.001 + 2.0 ** -24)
+    # blocks past the last one of a row have scale 0
+    blocks = K // ref.BLOCK[fmt]
+    assert np.all(ref.scale_bytes(q.scales, M, 4 * -(-blocks // 4))[:, blocks:] == 0)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K,b", [(2, 32, 32), (7, 96, 16), (65, 1152, 64), (40, 1152, 128), (9, 512, 256),
+                                   (3, 16384, 256), (12, 160, 2), (12, 160, 1), (200, 4608, 8)])
+@pytest.mark.parametrize("swap", [False, True])
+def test_quantize_rotated(fmt, M, K, b, swap):
+    """Inputs of few bits, so that the rotation is exact in fp32."""
+    g = gen(K + b)
+    X = (torch.randint(-64, 65, (M, K), generator=g, device=DEV) / 16).to(F16)
+    perm = perm_of(g, K) if swap else None
+    check_quantized(mx.quantize(X, fmt, perm, b), ref.hadamard(to64(X), perm, b))
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("M,K,b,swap", [(3, 96, 1, False), (130, 1536, 32, True)])
+def test_quantize_activation(fmt, act, M, K, b, swap):
+    g = gen(K)
+    X = rows_of(g, M, 2 * K if act == "swiglu" else K, BF16)
+    perm = perm_of(g, K) if swap else None
+    v = ref.hadamard(ref.act(to64(X), act), perm, b)
+    # the library's fp32 activation is within 2^-22 of |x|, and a rotation adds 32 of them: against
+    # a block's largest value less than 2^-18 at these sizes
+    check_quantized(mx.quantize(X, fmt, perm, b, act), v, slack=2.0 ** -18)
+
+
+def test_quantize_extremes():
+    K = 96
+    X = torch.zeros((6, K), dtype=BF16, device=DEV)
+    X[1, 40] = float("inf")
+    X[2, 3] = float("nan")
+    X[3] = torch.finfo(BF16).max
+    X[4] = 2.0 ** -126
+    X[5, :32] = 1e-30
+    q = mx.quantize(X, "block32")
+    byte = ref.scale_bytes(q.scales, 6, 3)
+    assert byte[1].tolist() == [0, 255, 0] and byte[2].tolist() == [255, 0, 0]
+    v = mx.dequantize(q)
+    assert v[1, 32:64].isnan().all() and v[2, :32].isnan().all() and (v[1, :32] == 0).all()
+    check_quantized(mx.quantize(X[3:], "block32"), to64(X[3:]))
+    q = mx.quantize(X, "block16")
+    v = mx.dequantize(q)
+    assert v[1].isnan().all() and v[2].isnan().all() and (v[0] == 0).all() and (v[4] == 0).all()
+    assert torch.isfinite(v[3]).all()
+
+
+def test_quantize_strides_and_views():
+    big = rows_of(gen(1), 50, 512, F16)
+    X = big[3:20, 64:320]
+    a, c = mx.quantize(X), mx.quantize(X.contiguous())
+    assert torch.equal(a.codes, c.codes)
+    np.testing.assert_array_equal(ref.scale_bytes(a.scales, 17, 8), ref.scale_bytes(c.scales, 17, 8))
+    assert mx.quantize(X[:0]).codes.shape == (0, 128)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K,N", [
+    (1, 32, 1), (1, 4096, 1000), (2, 64, 8), (31, 1184, 130), (32, 256, 128), (33, 288, 257), (127, 1152, 1152),
+    (128, 96, 1003), (129, 512, 64), (255, 2048, 384), (511, 320, 264), (512, 320, 264), (600, 1152, 129),
+    (1357, 1184, 1003), (2048, 4608, 1152), (513, 16384, 40)])
+def test_linear(fmt, M, K, N):
+    g = gen(M + N)
+    dtype = F16 if (M + N) % 2 else BF16
+    x = mx.quantize(rows_of(g, M, K, dtype), fmt)
+    w = mx.quantize((0.05 * torch.randn((N, K), generator=g, device=DEV)).to(dtype), fmt)
+    bias = torch.randn(N, generator=g, device=DEV).to(dtype) if N % 3 else None
+    xv, wv = ref.values_of(x), ref.values_of(w)
+    want = xv @ wv.T / 4
+    if bias is not None:
+        want = want + to64(bias)
+    got = to64(mx.linear(x, w, bias, 4, dtype))
+    bound = ref.product_bound(xv, wv, want, dtype, K)
+    assert np.all(np.abs(got - want) <= bound), np.abs((got - want) / bound).max()
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M", [1, 40, 700])
+def test_linear_exact_codes(fmt, M):
+    """Every code and many scales, sums that fp32 holds: the product is exact."""
+    K, N = 640, 200
+    g = gen(M)
+    def tensor(rows):
+        codes = torch.randint(0, 256, (rows, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+        # E8M0 2^-2 .. 2; E4M3 powers of two 2^-2 .. 2: sums of multiples of 2^-6 below 2^18
+        pick = torch.tensor([125, 126, 127, 128] if fmt == "block32" else [40, 48, 56, 64], dtype=torch.uint8, device=DEV)
+        scales = pick[torch.randint(0, 4, mx.scale_shape(rows, K, fmt), generator=g, device=DEV)]
+        rs = torch.full((rows,), 0.5, device=DEV) if fmt == "block16" else None
+        return mx.MXTensor(codes, scales, rs, fmt)
+    x, w = tensor(M), tensor(N)
+    want = ref.values_of(x) @ ref.values_of(w).T
+    got = mx.linear(x, w, dtype=F16)
+    wide = torch.from_numpy(want).float()
+    assert torch.equal(got.cpu(), wide.to(F16))
+
+
+def test_linear_nan_scale_stays_in_its_row():
+    X = rows_of(gen(3), 300, 256, BF16)
+    X[37, 100] = float("nan")
+    w = mx.quantize(rows_of(gen(4), 96, 256, BF16))
+    y = mx.linear(mx.quantize(X), w)
+    bad = y.isnan().any(1)
+    assert bad[37] and bad.sum() == 1 and y[37].isnan().all()
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,b", [(1, 64), (333, 128)])
+def test_layer_rotated_is_near_full_precision(fmt, M, b):
+    g = gen(b)
+    K, N = 1152, 480
+    X = rows_of(g, M, K, BF16)
+    W = (0.02 * torch.randn((N, K), generator=g, device=DEV)).to(BF16)
+    bias = torch.randn(N, generator=g, device=DEV).to(BF16)
+    layer = mx.MXLinear.from_weight(W, fmt, perm_of(g, K), b, bias)
+    y = to64(layer(X))
+    want = to64(X) @ to64(W).T + to64(bias)
+    # two operands of about 10 % quantization error each
+    assert np.linalg.norm(y - want) / np.linalg.norm(want - to64(bias)) < 0.2
+
+
+ROUTES = [
+    # T, E, k, scoring, balance, groups, top_groups, group_top
+    (1, 1, 1, "softmax", False, 1, 1, 2), (5, 8, 2, "softmax", False, 1, 1, 2), (33, 60, 4, "softmax", True, 4, 2, 2),
+    (64, 64, 6, "sigmoid", True, 8, 3, 2), (100, 160, 6, "softmax", False, 8, 3, 1), (257, 256, 8, "sigmoid", True, 8, 4, 2),
+    (31, 384, 8, "sigmoid", False, 1, 1, 2), (20, 512, 32, "softmax", False, 1, 1, 2), (9, 12, 12, "sigmoid", True, 12, 5, 2),
+]
+
+
+@pytest.mark.parametrize("case", ROUTES)
+@pytest.mark.parametrize("dtype", [torch.float32, F16, BF16])
+def test_route(case, dtype):
+    T, E, k, scoring, balance, groups, top_groups, group_top = case
+    g = gen(E)
+    logits = torch.randn((T, E + 3), generator=g, device=DEV).to(dtype)[:, :E]
+    logits[T // 2, ::2] = -float("inf")
+    logits[T // 3] = -float("inf")
+    bal = 0.1 * torch.randn(E, generator=g, device=DEV) if balance else None
+    r = mx.route(logits, k, scoring, bal, groups, top_groups, group_top, scale=2.5)
+    experts, weights, margin = ref.routing(to64(logits), None if bal is None else to64(bal), k, scoring, groups,
+                                           top_groups, group_top, scale=2.5)
+    # fp32 scores are within 2^-20 of the exact ones; a choice closer than that may fall either
+    # way, and scores of 16-bit logits tie exactly: there the lowest index is asked for
+    got = r.experts.cpu().numpy()
+    clear = (margin > 2.0 ** -20) | (margin == 0)
+    assert clear.mean() > 0.9
+    np.testing.assert_array_equal(got[clear], experts[clear])
+    np.testing.assert_allclose(r.weights.cpu().numpy()[clear], weights[clear], rtol=1e-5, atol=1e-9)
+
+
+def test_route_extremes():
+    inf, nan, big = float("inf"), float("nan"), torch.finfo(torch.float32).max
+    L = torch.tensor([[1.0, nan, 2.0, -inf], [-inf] * 4, [-big] * 4, [inf, 0, inf, 0], [nan] * 4, [3.0] * 4], device=DEV)
+    r = mx.route(L, 3)
+    assert r.experts.tolist() == [[2, 0, -1], [-1] * 3, [0, 1, 2], [0, 2, 1], [-1] * 3, [0, 1, 2]]
+    w = r.weights.cpu()
+    assert w[1].tolist() == [0, 0, 0] and w[4].tolist() == [0, 0, 0]
+    torch.testing.assert_close(w[2], torch.full((3,), 1 / 3))
+    torch.testing.assert_close(w[3], torch.tensor([0.5, 0.5, 0]))
+    s = mx.route(L, 3, "sigmoid", renormalize=False)
+    assert s.experts.tolist() == r.experts.tolist()
+    assert s.weights[3].tolist() == [1.0, 1.0, 0.5]
+    assert mx.route(L[:0], 2).experts.shape == (0, 2)
+
+
+@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 4, 64), (33, 2, 4), (500, 8, 60), (512, 3, 512), (513, 3, 512),
+                                   (3000, 4, 16), (9000, 2, 128)])
+def test_plan(T, k, E):
+    g = gen(T)
+    experts = torch.rand((T, E), generator=g, device=DEV).argsort(1)[:, :k].to(torch.int32)
+    experts[torch.rand((T, k), generator=g, device=DEV) < 0.1] = -1
+    r = mx.Routing(experts.contiguous(), torch.ones((T, k), device=DEV), E)
+    rows, space, R = mx.plan(r)
+    e, rows = experts.cpu().numpy(), rows.cpu().numpy()
+    want = np.full((T, k), -1)
+    start = 0
+    for x in range(E):
+        t, j = np.nonzero(e == x)
+        want[t, j] = start + np.arange(t.size)
+        start += -(-t.size // 128) * 128
+    np.testing.assert_array_equal(rows, want)
+    assert start <= R
+
+
+def experts_case(g, T, D, F, E, k, fmt, act, dtype, bias):
+    N1 = 2 * F if act == "swiglu" else F
+    W1 = (0.05 * torch.randn((E, N1, D), generator=g, device=DEV)).to(dtype)
+    W2 = (0.05 * torch.randn((E, D, F), generator=g, device=DEV)).to(dtype)
+    b1 = torch.randn((E, N1), generator=g, device=DEV).to(dtype) if bias else None
+    b2 = torch.randn((E, D), generator=g, device=DEV).to(dtype) if bias else None
+    return W1, W2, b1, b2
+
+
+@pytest.mark.parametrize("T,D,F,E,k,fmt,act,bias", [
+    (1, 256, 128, 8, 2, "block32", "swiglu", False), (7, 96, 64, 4, 4, "block16", "gelu", True),
+    (32, 288, 160, 16, 3, "block32", "gelu", True), (33, 512, 96, 60, 6, "block16", "swiglu", True),
+    (300, 1152, 288, 3, 2, "block32", "swiglu", True), (600, 256, 256, 5, 2, "block16", None, False),
+    (700, 320, 544, 8, 3, "block32", "swiglu", False), (2000, 128, 128, 2, 1, "block16", "gelu", True)])
+def test_experts(T, D, F, E, k, fmt, act, bias):
+    g = gen(T + E)
+    dtype = BF16 if T % 2 else F16
+    W1, W2, b1, b2 = experts_case(g, T, D, F, E, k, fmt, act, dtype, bias)
+    b = 32
+    perm = perm_of(g, D)
+    layer = mx.MXExperts.from_weights(W1, W2, fmt, act, perm, b, b1, b2)
+    X = rows_of(g, T, D, dtype)
+    logits = torch.randn((T, E), generator=g, device=DEV)
+    logits[T // 2] = -float("inf")  # a token that no expert takes
+    r = mx.route(logits, k)
+    y = to64(layer(X, r))
+    # step by step with the library's own quantized rows (checked above): products in 64 bits
+    x = ref.values_of(mx.quantize(X, fmt, perm, b))
+    e, w = r.experts.cpu().numpy(), to64(r.weights)
+    want, bound = np.zeros((T, D)), np.zeros((T, D))
+    eps = 2.0 ** -11 if dtype == F16 else 2.0 ** -8
+    for i in range(E):
+        t, j = np.nonzero(e == i)
+        if not t.size:
+            continue
+        pick = lambda s: mx.MXTensor(s.codes[i], s.scales[i], None if s.row_scale is None else s.row_scale[i], fmt)
+        w1, w2 = ref.values_of(pick(layer.w1)), ref.values_of(pick(layer.w2))
+        h = torch.from_numpy(x[t] @ w1.T / b + (to64(b1[i]) if bias else 0)).to(dtype)
+        a = ref.values_of(mx.quantize(h.to(DEV), fmt, act=act))
+        v = a @ w2.T + (to64(b2[i]) if bias else 0)
+        want[t] += w[t, j][:, None] * v
+        bound[t] += w[t, j][:, None] * (np.abs(v) * eps + 2.0 ** -24)
+    assert np.all(y[T // 2] == 0)
+    # h may round to the neighbouring 16-bit value, and its code then to the neighbouring one: rare,
+    # so most outputs agree to their rounding and all of them to a few percent of their size
+    off = np.abs(y - want)
+    close = off <= bound + eps * np.abs(want) + 1e-4 * np.sqrt(np.mean(want ** 2))
+    assert close.mean() > 0.9
+    assert np.linalg.norm(y - want) <= 1e-2 * np.linalg.norm(want)
+
+
+def test_combine_and_refusals():
+    g = gen(0)
+    Y = torch.randn((256, 64), generator=g, device=DEV).to(F16)
+    rows = torch.tensor([[3, -1], [255, 0]], dtype=torch.int32, device=DEV)
+    w = torch.tensor([[0.5, 9.0], [2.0, -1.0]], device=DEV)
+    out = torch.empty((2, 64), dtype=F16, device=DEV)
+    assert mx.clq_mx_combine(Y.data_ptr(), 0, rows.data_ptr(), w.data_ptr(), 2, 2, 64, 256, out.data_ptr(),
+                             torch.cuda.current_stream().cuda_stream) == 0
+    want = torch.stack([0.5 * Y[3].double(), 2 * Y[255].double() - Y[0].double()])
+    assert (out.double() - want).abs().max() <= 2.0 ** -10 * want.abs().max()
+
+
+def test_bad_indices_are_reported():
+    X = rows_of(gen(1), 4, 64, F16)
+    perm = torch.arange(64, dtype=torch.int32, device=DEV)
+    perm[5] = 64
+    mx.quantize(X, perm=perm)
+    assert clq.device_status() == 7
+    perm[5] = -1
+    mx.quantize(X, perm=perm)
+    assert clq.device_status() == 7
+
+
+def test_other_stream():
+    g = gen(5)
+    X, W = rows_of(g, 200, 512, BF16), rows_of(g, 256, 512, BF16)
+    layer = mx.MXLinear.from_weight(W)
+    want = layer(X)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = layer(X, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
