@@ -170,7 +170,10 @@ __device__ __forceinline__ void setup(Barriers* bars) {
   }
   if ((threadIdx.x >> 5) == WARP_MMA) {
     tmem_alloc<CG>(&bars->tmem_slot, C::TMEM);
-    tmem_relinquish<CG>();
+    // (a pair gives the permit up in teardown, when both CTAs have long allocated: given up
+    // by one of them while the other's allocation is on its way, it can leave that waiting
+    // for ever, as in a kernel of the same set-up once in 10^4 to 10^5 launches)
+    if (CG == 1) tmem_relinquish<CG>();
   }
 }
 
@@ -480,6 +483,7 @@ template <int CG = 1>
 __device__ __forceinline__ void teardown(uint32_t tmem, uint32_t cols) {
   if ((threadIdx.x >> 5) == WARP_MMA) {
     tc_fence_after();
+    if (CG == 2) tmem_relinquish<CG>();
     tmem_dealloc<CG>(tmem, cols);
   }
 }
