@@ -460,10 +460,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_after();
     tmem_dealloc<CG>(tmem, C::TMEM);
   }
-  if (CG == 2) {  // nor does a CTA of a pair leave before the other has deallocated
-    __syncwarp();
-    cluster_sync();
-  }
 }
 
 struct GemmMaps {
