@@ -99,7 +99,7 @@ def build(verbose=False, force=False, extra_flags=()):
     host_obj = _host_object()
     host_new = force or not os.path.exists(host_obj) or os.path.getmtime(host_obj) < max(
         os.path.getmtime(HOST_SRC),
-        os.path.getmtime(os.path.join(ROOT, "include", "clq.h")))
+        *(os.path.getmtime(h) for h in glob.glob(os.path.join(ROOT, "include", "*.h"))))
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     dep_t = _deps()
     jobs = []

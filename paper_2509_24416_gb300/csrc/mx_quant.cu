@@ -23,6 +23,17 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v) {
   return r;
 }
 
+// The values of the two codes in the low byte of w (the low nibble's first).
+__device__ __forceinline__ __half2 e2m1_pair(uint32_t w) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b;\n\t"
+      "mov.b16 {a, b}, %1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t}"
+      : "=r"(h)
+      : "h"(static_cast<uint16_t>(w)));
+  return *reinterpret_cast<const __half2*>(&h);
+}
+
 __device__ __forceinline__ uint32_t e4m3_byte(float v) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(v));
@@ -51,6 +62,13 @@ __device__ __forceinline__ void unpack8(const uint4& p, float* v) {
   }
 }
 
+// Largest absolute value, a NaN if one of them is.
+__device__ __forceinline__ float absmax3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // The activations, each operation rounded by itself.
 __device__ __forceinline__ float gelu(float x) {
   return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.f, erff(__fmul_rn(x, 0.70710678118654752f))));
@@ -59,72 +77,138 @@ __device__ __forceinline__ float swiglu(float g, float u) {
   return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.f, expf(-g))), u);
 }
 
+// A row's values as they are staged for the swap: the input's own 16 bits, or fp32 behind
+// an activation.
+template <typename T, int ACT>
+struct Staged {
+  using type = float;
+};
+template <typename T>
+struct Staged<T, CLQ_MX_ACT_NONE> {
+  using type = uint16_t;
+};
+
+// Where element e of a row is staged: one word is left out after every 32, so that the
+// lanes' reads of evenly spaced elements (a swap vector ascends in each half) fall on
+// different banks.
+template <typename S>
+__host__ __device__ __forceinline__ int staged_at(int e) {
+  constexpr int W = 4 / sizeof(S);  // elements a word
+  return e + W * (e / (32 * W));
+}
+template <typename S>
+__host__ __device__ __forceinline__ int staged_row(int K) {
+  return (staged_at<S>(K) + 7) / 8 * 8;
+}
+
 // blockDim.x threads a row (a multiple of 32; thread x holds values 16 x .. + 15),
-// blockDim.y rows at a time.
-template <typename T, int FMT, int ACT>
+// blockDim.y rows at a time.  One pass over X, bound by memory: the next row's loads are
+// issued before a row is worked on, and a row costs one barrier for its swap (two staging
+// buffers in turn) and one for its largest value (three slots in turn).
+template <typename T, int FMT, int ACT, bool SWAP>
 __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
-  extern __shared__ float stage[];  // [blockDim.y][K] with a swap vector
-  __shared__ uint32_t row_max[2][32];
+  using S = typename Staged<T, ACT>::type;
+  extern __shared__ __align__(16) uint8_t stage_raw[];  // SWAP: two rows of S for each y
+  __shared__ uint32_t row_max[3][32];
+  constexpr int NV = ACT == CLQ_MX_ACT_SWIGLU ? 4 : 2;  // 16-byte loads of a thread
   const int units = a.K / U;
   const int x = threadIdx.x, y = threadIdx.y, lane = x & 31;
   const bool on = x < units;
   const int chunks = scale_chunks(a.K, FMT);
+  if (FMT == CLQ_MX_BLOCK16) {
+    if (x < 3) row_max[x][y] = 0;
+    __syncthreads();
+  }
   pdl_wait();
   pdl_launch_dependents();
-  int src[U];
-  if (a.perm != nullptr && on) {
+  uint32_t src[SWAP ? U / 2 : 1];  // two 16-bit indices each
+  if (SWAP && on) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      int p = a.perm[x * U + i];
-      if (p < 0 || p >= a.K) {
-        record_status(a.status, CLQ_ERR_DEVICE_INDEX);
-        p = 0;
+    for (int i = 0; i < U; i += 4) {
+      int p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        p[j] = __ldg(a.perm + x * U + i + j);
+        if (p[j] < 0 || p[j] >= a.K) {
+          record_status(a.status, CLQ_ERR_DEVICE_INDEX);
+          p[j] = 0;
+        }
       }
-      src[i] = p;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = staged_at<S>(p[j]);
+      src[i / 2] = static_cast<uint32_t>(p[0] | (p[1] << 16));
+      src[i / 2 + 1] = static_cast<uint32_t>(p[2] | (p[3] << 16));
     }
   }
-  int turn = 0;
-  for (int r0 = blockIdx.x * blockDim.y; r0 < a.M; r0 += gridDim.x * blockDim.y, turn ^= 1) {
+  const int step = gridDim.x * blockDim.y;
+  uint4 raw[NV];
+  auto fetch = [&](int row) {
+    if (on && row < a.M) {
+      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.X) +
+                                                      static_cast<size_t>(row) * a.ld) +
+                       static_cast<size_t>(x) * NV;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i] = __ldg(p + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) raw[i] = make_uint4(0, 0, 0, 0);
+    }
+  };
+  fetch(blockIdx.x * blockDim.y + y);
+  int turn = 0, slot = 0;
+  for (int r0 = blockIdx.x * blockDim.y; r0 < a.M; r0 += step, turn ^= 1) {
     const int row = r0 + y;
     const bool live = on && row < a.M;
     float v[U];
+    if constexpr (ACT == CLQ_MX_ACT_SWIGLU) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = 0.f;
-    if (live) {
-      const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.X) +
-                                                      static_cast<size_t>(row) * a.ld) +
-                       static_cast<size_t>(x) * (ACT == CLQ_MX_ACT_SWIGLU ? 4 : 2);
-      if (ACT == CLQ_MX_ACT_SWIGLU) {
+      for (int h = 0; h < 2; ++h) {
+        float g[8], u[8];
+        unpack8<T>(raw[2 * h], g);
+        unpack8<T>(raw[2 * h + 1], u);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float g[8], u[8];
-          unpack8<T>(__ldg(p + 2 * h), g);
-          unpack8<T>(__ldg(p + 2 * h + 1), u);
+        for (int i = 0; i < 8; ++i) v[8 * h + i] = swiglu(g[i], u[i]);
+      }
+    } else if constexpr (ACT == CLQ_MX_ACT_GELU || !SWAP) {
+      unpack8<T>(raw[0], v);
+      unpack8<T>(raw[1], v + 8);
+      if (ACT == CLQ_MX_ACT_GELU) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[8 * h + i] = swiglu(g[i], u[i]);
-        }
-      } else {
-        unpack8<T>(__ldg(p), v);
-        unpack8<T>(__ldg(p + 1), v + 8);
-        if (ACT == CLQ_MX_ACT_GELU) {
-#pragma unroll
-          for (int i = 0; i < U; ++i) v[i] = gelu(v[i]);
-        }
+        for (int i = 0; i < U; ++i) v[i] = gelu(v[i]);
       }
     }
-    if (a.perm != nullptr) {
-      float* s = stage + static_cast<size_t>(y) * a.K;
-      if (live) {
+    if constexpr (SWAP) {
+      S* s = reinterpret_cast<S*>(stage_raw) +
+             static_cast<size_t>(turn * blockDim.y + y) * staged_row<S>(a.K);
+      if (on) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(s + staged_at<S>(x * U));
+        if constexpr (ACT == CLQ_MX_ACT_NONE) {
+          const uint32_t r[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w,
+                                 raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-        for (int i = 0; i < U; i += 4)
-          *reinterpret_cast<float4*>(s + x * U + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-      }
-      __syncthreads();
-      if (live) {
+          for (int i = 0; i < 8; ++i) w[i] = r[i];
+        } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) v[i] = s[src[i]];
+          for (int i = 0; i < U; ++i) w[i] = __float_as_uint(v[i]);
+        }
       }
+      fetch(row + step);
       __syncthreads();
+      if (on) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const S e = s[(src[i / 2] >> (16 * (i & 1))) & 0xFFFFu];
+          if constexpr (ACT == CLQ_MX_ACT_NONE)
+            v[i] = Num<T>::to_f(e);
+          else
+            v[i] = e;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i) v[i] = 0.f;
+      }
+    } else {
+      fetch(row + step);
     }
     // H_b: stages 1, 2, 4, 8 in a thread's values, 16 and up between lanes (K % b ==
     // 0, so the b / 16 lanes of a block are neighbours, all on or all off).
@@ -141,48 +225,54 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       }
     }
     for (int m = 1; m * U < a.b; m *= 2) {
+      // o + v or o - v as one fused operation: the product with 1 or -1 is exact
+      const float sign = (lane & m) ? -1.f : 1.f;
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const float o = __shfl_xor_sync(0xffffffffu, v[i], m);
-        v[i] = (lane & m) ? __fsub_rn(o, v[i]) : __fadd_rn(v[i], o);
+      for (int i = 0; i < U; i += 2) {
+        const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, v[i], m),
+                                     __shfl_xor_sync(0xffffffffu, v[i + 1], m));
+        const float2 r = __ffma2_rn(make_float2(v[i], v[i + 1]), make_float2(sign, sign), o);
+        v[i] = r.x;
+        v[i + 1] = r.y;
       }
     }
-    // Largest absolute value by its bits: a NaN's are above an infinity's.
-    uint32_t amax = 0;
+    // Largest absolute value; from here on by its bits, a NaN's being above an infinity's.
+    float most = fabsf(v[0]);
 #pragma unroll
-    for (int i = 0; i < U; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    for (int i = 1; i + 1 < U; i += 2) most = absmax3(most, v[i], v[i + 1]);
+    most = absmax3(most, v[U - 1], v[U - 1]);
+    uint32_t amax = __float_as_uint(most);
     uint32_t byte;
     float inv, srow = 0.f;
+    bool bad;
     if (FMT == CLQ_MX_BLOCK32) {
       amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
       const int e = static_cast<int>(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
-      const bool bad = amax >= 0x7F800000u;
+      bad = amax >= 0x7F800000u;
       byte = bad ? 255u : static_cast<uint32_t>(max(e, 0));
-      inv = bad ? 0.f : __uint_as_float((254u - byte) << 23);
-      if (bad) {
-#pragma unroll
-        for (int i = 0; i < U; ++i) v[i] = 0.f;
-      }
+      inv = __uint_as_float((254u - byte) << 23);
     } else {
-      if (x == 0) row_max[turn][y] = 0;
-      __syncthreads();
       const uint32_t wmax = __reduce_max_sync(0xffffffffu, amax);
-      if (lane == 0 && wmax != 0) atomicMax(&row_max[turn][y], wmax);
+      if (lane == 0 && wmax != 0) atomicMax(&row_max[slot][y], wmax);
       __syncthreads();
-      const uint32_t rmax = row_max[turn][y];
-      const bool bad = rmax >= 0x7F800000u;
+      const uint32_t rmax = row_max[slot][y];
+      slot = slot == 2 ? 0 : slot + 1;
+      // used again in two rows' time, behind the next row's barrier
+      if (x == 0) row_max[slot == 2 ? 0 : slot + 1][y] = 0;
+      bad = rmax >= 0x7F800000u;
       srow = bad ? __uint_as_float(0x7FC00000u)
                  : fmaxf(__fmul_rn(__uint_as_float(rmax), 1.f / 2688.f), 0x1p-100f);
       byte = bad ? 0u : e4m3_byte(__fdiv_rn(__uint_as_float(amax), __fmul_rn(6.f, srow)));
       inv = byte == 0 ? 0.f : __fdiv_rn(1.f, __fmul_rn(e4m3_value(byte), srow));
-      if (bad) {
-#pragma unroll
-        for (int i = 0; i < U; ++i) v[i] = 0.f;
-      }
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) v[i] = __fmul_rn(v[i], inv);
-    const uint2 q = make_uint2(e2m1x8(v), e2m1x8(v + 8));
+    for (int i = 0; i < U; i += 2) {
+      const float2 r = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(inv, inv));
+      v[i] = r.x;
+      v[i + 1] = r.y;
+    }
+    uint2 q = make_uint2(e2m1x8(v), e2m1x8(v + 8));
+    if (bad) q = make_uint2(0, 0);
     // Four scales a word: those of this lane and of three lanes (pairs) behind it.
     if (!on) byte = 0;
     constexpr int STEP = FMT == CLQ_MX_BLOCK32 ? 2 : 1;
@@ -211,58 +301,51 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
   }
 }
 
-// One thread 16 codes of a row.
+// One thread eight codes of a row, so that a warp's stores are whole lines; blockDim.y rows
+// at a time.
 template <typename T, int FMT>
-__global__ void dequantize_kernel(const uint8_t* __restrict__ codes,
-                                  const uint8_t* __restrict__ scales,
-                                  const float* __restrict__ row_scale, int M, int K, T* out) {
-  const int units = K / U;
+__global__ void __launch_bounds__(256)
+    dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                      const float* __restrict__ row_scale, int M, int K, T* out) {
+  const int units = K / 8;
   const int chunks = scale_chunks(K, FMT);
-  const size_t n = static_cast<size_t>(M) * units;
   pdl_wait();
   pdl_launch_dependents();
-  for (size_t i = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x; i < n;
-       i += static_cast<size_t>(gridDim.x) * blockDim.x) {
-    const int row = static_cast<int>(i / units);
-    const int x = static_cast<int>(i - static_cast<size_t>(row) * units);
-    const int blk = FMT == CLQ_MX_BLOCK32 ? x >> 1 : x;
-    const uint32_t byte = scales[(static_cast<size_t>(row / kRowBlock) * chunks + (blk >> 2)) * 512 +
-                                 (row & 31) * 16 + ((row >> 5) & 3) * 4 + (blk & 3)];
-    const float s = FMT == CLQ_MX_BLOCK32 ? e8m0_value(byte) : e4m3_value(byte);
-    const float r = FMT == CLQ_MX_BLOCK32 ? 1.f : row_scale[row];
-    const uint2 q = reinterpret_cast<const uint2*>(codes)[i];
-    uint32_t o[8];
+  for (int row = blockIdx.x * blockDim.y + threadIdx.y; row < M; row += gridDim.x * blockDim.y) {
+    const uint8_t* sc = scales + static_cast<size_t>(row / kRowBlock) * chunks * 512 +
+                        (row & 31) * 16 + ((row >> 5) & 3) * 4;
+    const float r = FMT == CLQ_MX_BLOCK32 ? 1.f : __ldg(row_scale + row);
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(codes) + static_cast<size_t>(row) * units;
+    uint4* dst = reinterpret_cast<uint4*>(out) + static_cast<size_t>(row) * units;
+#pragma unroll 4
+    for (int x = threadIdx.x; x < units; x += blockDim.x) {
+      const uint32_t w = __ldg(q + x);
+      const int blk = FMT == CLQ_MX_BLOCK32 ? x >> 2 : x >> 1;
+      const uint32_t byte = __ldg(sc + (blk >> 2) * 512 + (blk & 3));
+      const float s = FMT == CLQ_MX_BLOCK32 ? e8m0_value(byte) : e4m3_value(byte);
+      uint32_t o[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float v[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t c = ((j < 4 ? q.x : q.y) >> (8 * (j & 3) + 4 * h)) & 15u;
-        const uint32_t m = c & 7u;
-        const float mag = 0.25f * static_cast<float>(m < 2 ? 2 * m : (2 + (m & 1)) << (m >> 1));
+      for (int j = 0; j < 4; ++j) {
         // code times block scale is exact; one rounding by the row scale, one by T
-        v[h] = __fmul_rn(__fmul_rn((c & 8u) ? -mag : mag, s), r);
+        float2 v = __half22float2(e2m1_pair(w >> (8 * j)));
+        v = __fmul2_rn(v, make_float2(s, s));
+        if (FMT == CLQ_MX_BLOCK16) v = __fmul2_rn(v, make_float2(r, r));
+        o[j] = Num<T>::pack2(v.x, v.y);
       }
-      o[j] = Num<T>::pack2(v[0], v[1]);
+      dst[x] = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    uint4* dst = reinterpret_cast<uint4*>(out) + 2 * i;
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
-template <typename T, int FMT>
-cudaError_t quantize_t(const QuantArgs& a, cudaStream_t st) {
-  const int tx = (a.K / U + 31) / 32 * 32;
-  const int ty = std::max(1, std::min(32, 256 / tx));
-  const size_t smem = a.perm != nullptr ? static_cast<size_t>(ty) * a.K * 4 : 0;
-  void (*k)(QuantArgs) = a.act == CLQ_MX_ACT_GELU     ? quantize_kernel<T, FMT, CLQ_MX_ACT_GELU>
-                         : a.act == CLQ_MX_ACT_SWIGLU ? quantize_kernel<T, FMT, CLQ_MX_ACT_SWIGLU>
-                                                      : quantize_kernel<T, FMT, CLQ_MX_ACT_NONE>;
-  int per_sm = 0;
-  cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, tx * ty, &per_sm);
-  if (e != cudaSuccess) return e;
-  const int grid = std::min((a.M + ty - 1) / ty, std::max(1, per_sm) * sm_count());
+template <typename T, int FMT, int ACT>
+auto pick(const int32_t* perm) {
+  return perm != nullptr ? quantize_kernel<T, FMT, ACT, true> : quantize_kernel<T, FMT, ACT, false>;
+}
+
+// A launch of tx x ty threads that may start while the previous kernel finishes.
+template <typename... KArgs, typename... Args>
+cudaError_t launch_rows(void (*k)(KArgs...), int grid, int tx, int ty, size_t smem, cudaStream_t st,
+                        Args... args) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -273,16 +356,36 @@ cudaError_t quantize_t(const QuantArgs& a, cudaStream_t st) {
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k, a);
+  return cudaLaunchKernelEx(&cfg, k, args...);
+}
+
+template <typename T, int FMT>
+cudaError_t quantize_t(const QuantArgs& a, cudaStream_t st) {
+  const int tx = (a.K / U + 31) / 32 * 32;
+  const int ty = std::max(1, std::min(32, 256 / tx));
+  const size_t smem = a.perm == nullptr ? 0
+                      : a.act == CLQ_MX_ACT_NONE
+                          ? static_cast<size_t>(2 * ty) * staged_row<uint16_t>(a.K) * 2
+                          : static_cast<size_t>(2 * ty) * staged_row<float>(a.K) * 4;
+  void (*k)(QuantArgs) =
+      a.act == CLQ_MX_ACT_GELU     ? pick<T, FMT, CLQ_MX_ACT_GELU>(a.perm)
+      : a.act == CLQ_MX_ACT_SWIGLU ? pick<T, FMT, CLQ_MX_ACT_SWIGLU>(a.perm)
+                                   : pick<T, FMT, CLQ_MX_ACT_NONE>(a.perm);
+  int per_sm = 0;
+  cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, tx * ty, &per_sm);
+  if (e != cudaSuccess) return e;
+  const int grid = std::min((a.M + ty - 1) / ty, std::max(1, per_sm) * sm_count());
+  return launch_rows(k, grid, tx, ty, smem, st, a);
 }
 
 template <typename T, int FMT>
 cudaError_t dequantize_t(const uint8_t* codes, const uint8_t* scales, const float* row_scale,
                          int M, int K, void* out, cudaStream_t st) {
-  const size_t n = static_cast<size_t>(M) * (K / U);
-  const int grid = static_cast<int>(std::min<size_t>((n + 255) / 256, 8u * sm_count()));
-  return launch_pdl(dequantize_kernel<T, FMT>, grid, 256, 0, st, codes, scales, row_scale, M, K,
-                    static_cast<T*>(out));
+  const int tx = std::min(256, (K / 8 + 31) / 32 * 32);
+  const int ty = 256 / tx;
+  const int grid = std::min((M + ty - 1) / ty, 8 * sm_count());
+  return launch_rows(dequantize_kernel<T, FMT>, grid, tx, ty, 0, st, codes, scales, row_scale, M, K,
+                     static_cast<T*>(out));
 }
 
 }  // namespace

@@ -20,6 +20,7 @@ BLOCK32, BLOCK16 = 0, 1
 FORMATS = {"block32": BLOCK32, "block16": BLOCK16}
 ACTS = {"none": 0, None: 0, "gelu": 1, "swiglu": 2}
 SCORING = {"softmax": 0, "sigmoid": 1}
+DTYPES = {torch.float16: clq.CLQ_F16, torch.bfloat16: clq.CLQ_BF16}
 CLQ_F32 = 2
 
 _P, _I, _Z, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
@@ -138,11 +139,30 @@ class MXTensor:
         self.codes, self.scales, self.row_scale, self.fmt = codes, scales, row_scale, fmt
         self.rows, self.K = rows, K
 
+    @classmethod
+    def _made(cls, codes, scales, row_scale, fmt):
+        """Around arrays that a call of this module has just made."""
+        t = cls.__new__(cls)
+        t.codes, t.scales, t.row_scale, t.fmt = codes, scales, row_scale, fmt
+        t.rows, t.K = codes.shape[0], 2 * codes.shape[1]
+        return t
+
 
 def _empty(rows, K, fmt, device):
     return (torch.empty((rows, K // 2), dtype=torch.uint8, device=device),
             torch.empty(scale_shape(rows, K, fmt), dtype=torch.uint8, device=device),
             torch.empty(rows, dtype=torch.float32, device=device) if fmt == "block16" else None)
+
+
+def _native(name, *args, where):
+    """The native form of a call (module _clq_host): its result, or None where it does not take
+    these arguments or the module is missing.  `where`: the C calls its status may be of."""
+    host = clq._host or clq._find_host()
+    fn = getattr(host, name, None) if host else None
+    r = fn(*args) if fn is not None else None
+    if type(r) is int:
+        raise clq.ClqError(r & 255, where[r >> 8])
+    return r
 
 
 def _row_input(X, act, perm):
@@ -167,13 +187,16 @@ def quantize(X, fmt="block32", perm=None, b=1, act=None, stream=None):
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, quantize, X, fmt, perm, b, act)
     f = _format(fmt)
+    r = _native("mx_quantize", X, f, perm, b, ACTS.get(act, -1), where=("clq_mx_quantize",))
+    if r is not None:
+        return MXTensor._made(*r, fmt)
     K = _row_input(X, act, perm)
     M = X.shape[0]
     codes, scales, rows = _empty(M, K, fmt, X.device)
     _check(clq_mx_quantize(_ptr(X), _dt(X), M, K, X.stride(0), _ptr(perm), b, ACTS[act], f,
                            _ptr(codes), _ptr(scales), _ptr(rows), None, 0, M, _stream(stream)),
            "clq_mx_quantize")
-    return MXTensor(codes, scales, rows, fmt)
+    return MXTensor._made(codes, scales, rows, fmt)
 
 
 def dequantize(q, dtype=torch.bfloat16, stream=None):
@@ -182,6 +205,11 @@ def dequantize(q, dtype=torch.bfloat16, stream=None):
         return _with_stream(stream, dequantize, q, dtype)
     if q.codes.dim() != 2:
         raise ValueError("expected one array of rows, got a stack")
+    if dtype in DTYPES:
+        r = _native("mx_dequantize", q.codes, q.scales, q.row_scale, FORMATS[q.fmt], DTYPES[dtype],
+                    where=("clq_mx_dequantize",))
+        if r is not None:
+            return r
     out = torch.empty((q.rows, q.K), dtype=dtype, device=q.codes.device)
     _check(clq_mx_dequantize(_ptr(q.codes), _ptr(q.scales), _ptr(q.row_scale), q.rows, q.K,
                              _format(q.fmt), _dt(out), _ptr(out), _stream(stream)),
@@ -232,6 +260,12 @@ class MXLinear:
         """Y = act(X) W^T + bias, X [M, K] (or [M, 2K], see quantize)."""
         if stream is not None and _elsewhere(stream):
             return _with_stream(stream, self, X, act, Y)
+        w = self.w
+        if Y is None:
+            r = _native("mx_layer", X, FORMATS[w.fmt], self.perm, self.b, ACTS.get(act, -1), w.codes,
+                        w.scales, w.row_scale, self.bias, where=("clq_mx_quantize", "clq_mx_linear"))
+            if r is not None:
+                return r
         q = quantize(X, self.w.fmt, self.perm, self.b, act)
         return linear(q, self.w, self.bias, self.b, X.dtype, Y)
 
@@ -246,6 +280,12 @@ class Routing:
         _on(weights, torch.float32, experts.device, "weights")
         self.experts, self.weights, self.E = experts, weights, E
 
+    @classmethod
+    def _made(cls, experts, weights, E):
+        r = cls.__new__(cls)
+        r.experts, r.weights, r.E = experts, weights, E
+        return r
+
 
 def route(logits, k, scoring="softmax", balance=None, groups=1, top_groups=1, group_top=2,
           renormalize=True, scale=1.0, stream=None):
@@ -254,9 +294,13 @@ def route(logits, k, scoring="softmax", balance=None, groups=1, top_groups=1, gr
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, route, logits, k, scoring, balance, groups, top_groups,
                             group_top, renormalize, scale)
-    _row_major(logits, "logits")
     if scoring not in SCORING:
         raise ValueError("scoring must be one of %s, got %r" % (sorted(SCORING), scoring))
+    r = _native("mx_route", logits, k, SCORING[scoring], balance, groups, top_groups, group_top,
+                int(renormalize), scale, where=("clq_mx_route",))
+    if r is not None:
+        return Routing._made(*r, logits.shape[1])
+    _row_major(logits, "logits")
     T, E = logits.shape
     _on(balance, torch.float32, logits.device, "balance")
     if balance is not None and tuple(balance.shape) != (E,):
@@ -267,7 +311,7 @@ def route(logits, k, scoring="softmax", balance=None, groups=1, top_groups=1, gr
     _check(clq_mx_route(_ptr(logits), dtype, T, E, logits.stride(0), _ptr(balance), k,
                         SCORING[scoring], groups, top_groups, group_top, int(renormalize), scale,
                         _ptr(experts), _ptr(weights), _stream(stream)), "clq_mx_route")
-    return Routing(experts, weights, E)
+    return Routing._made(experts, weights, E)
 
 
 def plan(routing, stream=None):
@@ -329,6 +373,15 @@ class MXExperts:
         """X [T, K], routing of its tokens -> [T, N] in X's type."""
         if stream is not None and _elsewhere(stream):
             return _with_stream(stream, self, X, routing)
+        w1, w2 = self.w1, self.w2
+        if routing.E == self.E:
+            r = _native("mx_experts", X, routing.experts, routing.weights, FORMATS[w1.fmt], self.perm,
+                        self.b, ACTS[self.act], w1.codes, w1.scales, w1.row_scale, self.bias1,
+                        w2.codes, w2.scales, w2.row_scale, self.bias2,
+                        where=("clq_mx_plan", "clq_mx_quantize", "clq_mx_grouped_linear",
+                               "clq_mx_combine"))
+            if r is not None:
+                return r
         K = _row_input(X, None, self.perm)
         T, k = routing.experts.shape
         if K != self.w1.K or X.shape[0] != T or routing.E != self.E:
