@@ -145,6 +145,28 @@ clq_status clq_mx_grouped_linear(const uint8_t* Xq, const uint8_t* Xs, const flo
                                  clq_dtype dtype, void* Y, void* stream);
 
 /*
+ * The same product in blocks of 32, with its output as the next product's operand: h =
+ * out_dtype(x w^T / b + bias) as clq_mx_grouped_linear would store it, then act(h), here
+ * within 2^-20 |h| of its value (of |g u| for SWIGLU), quantized as by clq_mx_quantize, into Yq / Ys: codes and scales of clq_mx_plan_rows
+ * rows of N codes (N / 2 for SWIGLU), N % 32 == 0 (64 for SWIGLU), at most 16384 codes.
+ */
+clq_status clq_mx_grouped_linear_act(const uint8_t* Xq, const uint8_t* Xs, const void* plan,
+                                     const uint8_t* Wq, const uint8_t* Ws, const void* bias,
+                                     int32_t T, int32_t k, int32_t E, int32_t N, int32_t K,
+                                     int32_t b, clq_dtype dtype, clq_mx_act act, uint8_t* Yq,
+                                     uint8_t* Ys, void* stream);
+
+/*
+ * The rows of a plan, act(X) without swap or rotation -> codes and scales: what
+ * clq_mx_quantize makes of the rows that tokens have, the others undefined.  X: device
+ * [clq_mx_plan_rows][ldx].
+ */
+clq_status clq_mx_quantize_rows(const void* X, clq_dtype dtype, const void* plan, int32_t T,
+                                int32_t k, int32_t E, int32_t K, int32_t ldx, clq_mx_act act,
+                                clq_mx_format fmt, uint8_t* codes, uint8_t* scales,
+                                float* row_scale, void* stream);
+
+/*
  * out[t] = sum_j weights[t][j] Y[rows[t][j]] over the places with rows >= 0, in
  * the order of j, in fp32.  Y: device [R][D] of `dtype`, D % 8 == 0; out: [T][D].
  */

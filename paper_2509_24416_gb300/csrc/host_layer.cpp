@@ -17,8 +17,6 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
-#include <algorithm>
-
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -350,7 +348,7 @@ PyObject* mx_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   int32_t* rows = static_cast<int32_t*>(plan.data_ptr());
   void* space = plan.data_ptr<uint8_t>() + row_bytes;
   const Space x(R, K, fmt, *X), h(R, F, fmt, *X);
-  const at::Tensor Y = at::empty({R, std::max(N, N1)}, X->options());
+  const at::Tensor Y = at::empty({R, N}, X->options());
   const clq_mx_format f = static_cast<clq_mx_format>(fmt);
   const clq_dtype dt = dtype_of(*X);
   void* st = current_stream();
@@ -360,13 +358,21 @@ PyObject* mx_experts(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                       data<int32_t>(perm), static_cast<int32_t>(b), CLQ_MX_ACT_NONE, f, x.codes,
                       x.scales, x.row_scale, rows, k, R, st);
   if (r != CLQ_OK) return status_of(r, 1);
-  r = unlocked(clq_mx_grouped_linear, x.codes, x.scales, x.row_scale, space, data<uint8_t>(q1),
-                            data<uint8_t>(s1), data<float>(r1), data<void>(bias1), T, k, E, N1, K,
-                            static_cast<int32_t>(b), f, dt, Y.data_ptr(), st);
-  if (r != CLQ_OK) return status_of(r, 2);
-  r = unlocked(clq_mx_quantize, Y.data_ptr(), dt, R, F, N1, nullptr, 1, static_cast<clq_mx_act>(act), f,
-                      h.codes, h.scales, h.row_scale, nullptr, 0, R, st);
-  if (r != CLQ_OK) return status_of(r, 1);
+  if (f == CLQ_MX_BLOCK32) {
+    r = unlocked(clq_mx_grouped_linear_act, x.codes, x.scales, space, data<uint8_t>(q1),
+                 data<uint8_t>(s1), data<void>(bias1), T, k, E, N1, K, static_cast<int32_t>(b), dt,
+                 static_cast<clq_mx_act>(act), h.codes, h.scales, st);
+    if (r != CLQ_OK) return status_of(r, 4);
+  } else {  // a row's scale needs the whole row
+    const at::Tensor H = at::empty({R, N1}, X->options());
+    r = unlocked(clq_mx_grouped_linear, x.codes, x.scales, x.row_scale, space, data<uint8_t>(q1),
+                 data<uint8_t>(s1), data<float>(r1), data<void>(bias1), T, k, E, N1, K,
+                 static_cast<int32_t>(b), f, dt, H.data_ptr(), st);
+    if (r != CLQ_OK) return status_of(r, 2);
+    r = unlocked(clq_mx_quantize_rows, H.data_ptr(), dt, space, T, k, E, F, N1,
+                 static_cast<clq_mx_act>(act), f, h.codes, h.scales, h.row_scale, st);
+    if (r != CLQ_OK) return status_of(r, 5);
+  }
   r = unlocked(clq_mx_grouped_linear, h.codes, h.scales, h.row_scale, space, data<uint8_t>(q2),
                             data<uint8_t>(s2), data<float>(r2), data<void>(bias2), T, k, E, N, F, 1,
                             f, dt, Y.data_ptr(), st);

@@ -33,6 +33,46 @@ bool valid_routing(int T, int k, int E) {
          static_cast<int64_t>(T) * k + 128ll * E < (1ll << 31);
 }
 
+// The experts' products, their output in Y or, behind `act`, as codes in Yq / Ys.
+clq_status grouped(const uint8_t* Xq, const uint8_t* Xs, const float* s_x, const void* plan,
+                   const uint8_t* Wq, const uint8_t* Ws, const float* s_w, const void* bias, int T,
+                   int k, int E, int N, int K, int b, int fmt, int dtype, void* Y, int act,
+                   uint8_t* Yq, uint8_t* Ys, void* stream) {
+  if (!valid_dtype(dtype) || !valid_format(fmt) || N < 0) return CLQ_ERR_INVALID_ARG;
+  if (!valid_k(K) || !valid_b(b, K) || !valid_routing(T, k, E) ||
+      static_cast<int64_t>(E) * N >= (1ll << 31))
+    return CLQ_ERR_SHAPE;
+  if (T == 0 || N == 0) return CLQ_OK;
+  if ((Y == nullptr && Yq == nullptr) || plan == nullptr) return CLQ_ERR_INVALID_ARG;
+  if (!aligned(Y, 16) || !aligned(plan, 16) || (bias != nullptr && !aligned(bias, 2)))
+    return CLQ_ERR_ALIGN;
+  clq_status st = check_codes(Xq, Xs, s_x, fmt, 4);
+  if (st == CLQ_OK) st = check_codes(Wq, Ws, s_w, fmt, 4);
+  if (st != CLQ_OK) return st;
+  mx::GemmArgs g{};
+  if ((st = device_status(&g.status)) != CLQ_OK) return st;
+  const mx::PlanLayout pl = mx::plan_layout(T, k, E);
+  g.s_x = s_x;
+  g.s_w = s_w;
+  g.bias = bias;
+  g.Y = Y;
+  g.Yq = Yq;
+  g.Ys = Ys;
+  g.act = act;
+  if (Yq != nullptr)
+    g.y_chunks = mx::scale_chunks(act == CLQ_MX_ACT_SWIGLU ? N / 2 : N, CLQ_MX_BLOCK32);
+  g.x_rows = mx::plan_rows(T, k, E);
+  g.M = g.x_rows;
+  g.N = N;
+  g.K = K;
+  g.inv_b = 1.0f / static_cast<float>(b);
+  g.chunks = mx::scale_chunks(K, fmt);
+  g.w_blocks = (N + mx::kRowBlock - 1) / mx::kRowBlock;
+  g.experts = E;
+  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, plan, &pl, T,
+                                   static_cast<cudaStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -188,34 +228,54 @@ clq_status clq_mx_grouped_linear(const uint8_t* Xq, const uint8_t* Xs, const flo
                                  const float* s_w, const void* bias, int32_t T, int32_t k,
                                  int32_t E, int32_t N, int32_t K, int32_t b, clq_mx_format fmt,
                                  clq_dtype dtype, void* Y, void* stream) {
-  if (!valid_dtype(dtype) || !valid_format(fmt) || N < 0) return CLQ_ERR_INVALID_ARG;
-  if (!valid_k(K) || !valid_b(b, K) || !valid_routing(T, k, E) ||
-      static_cast<int64_t>(E) * N >= (1ll << 31))
+  return grouped(Xq, Xs, s_x, plan, Wq, Ws, s_w, bias, T, k, E, N, K, b, fmt, dtype, Y,
+                 CLQ_MX_ACT_NONE, nullptr, nullptr, stream);
+}
+
+clq_status clq_mx_grouped_linear_act(const uint8_t* Xq, const uint8_t* Xs, const void* plan,
+                                     const uint8_t* Wq, const uint8_t* Ws, const void* bias,
+                                     int32_t T, int32_t k, int32_t E, int32_t N, int32_t K,
+                                     int32_t b, clq_dtype dtype, clq_mx_act act, uint8_t* Yq,
+                                     uint8_t* Ys, void* stream) {
+  if (act < CLQ_MX_ACT_NONE || act > CLQ_MX_ACT_SWIGLU) return CLQ_ERR_INVALID_ARG;
+  const bool gated = act == CLQ_MX_ACT_SWIGLU;
+  if (N > 0 && (N % (gated ? 64 : 32) != 0 || !valid_k(gated ? N / 2 : N))) return CLQ_ERR_SHAPE;
+  if (T > 0 && N > 0 && (Yq == nullptr || Ys == nullptr)) return CLQ_ERR_INVALID_ARG;
+  if (!aligned(Yq, 16) || !aligned(Ys, 16)) return CLQ_ERR_ALIGN;
+  return grouped(Xq, Xs, nullptr, plan, Wq, Ws, nullptr, bias, T, k, E, N, K, b, CLQ_MX_BLOCK32,
+                 dtype, nullptr, act, Yq, Ys, stream);
+}
+
+clq_status clq_mx_quantize_rows(const void* X, clq_dtype dtype, const void* plan, int32_t T,
+                                int32_t k, int32_t E, int32_t K, int32_t ldx, clq_mx_act act,
+                                clq_mx_format fmt, uint8_t* codes, uint8_t* scales,
+                                float* row_scale, void* stream) {
+  if (!valid_dtype(dtype) || !valid_format(fmt) || act < CLQ_MX_ACT_NONE || act > CLQ_MX_ACT_SWIGLU)
+    return CLQ_ERR_INVALID_ARG;
+  if (!valid_k(K) || !valid_routing(T, k, E) || ldx < (act == CLQ_MX_ACT_SWIGLU ? 2ll * K : K))
     return CLQ_ERR_SHAPE;
-  if (T == 0 || N == 0) return CLQ_OK;
-  if (Y == nullptr || plan == nullptr) return CLQ_ERR_INVALID_ARG;
-  if (!aligned(Y, 16) || !aligned(plan, 16) || (bias != nullptr && !aligned(bias, 2)))
-    return CLQ_ERR_ALIGN;
-  clq_status st = check_codes(Xq, Xs, s_x, fmt, 4);
-  if (st == CLQ_OK) st = check_codes(Wq, Ws, s_w, fmt, 4);
+  if (ldx % 8 != 0) return CLQ_ERR_ALIGN;
+  if (T == 0) return CLQ_OK;
+  if (X == nullptr || plan == nullptr) return CLQ_ERR_INVALID_ARG;
+  if (!aligned(X, 16) || !aligned(plan, 16)) return CLQ_ERR_ALIGN;
+  clq_status st = check_codes(codes, scales, row_scale, fmt, 4);
   if (st != CLQ_OK) return st;
-  mx::GemmArgs g{};
-  if ((st = device_status(&g.status)) != CLQ_OK) return st;
+  mx::QuantArgs a{};
+  if ((st = device_status(&a.status)) != CLQ_OK) return st;
   const mx::PlanLayout pl = mx::plan_layout(T, k, E);
-  g.s_x = s_x;
-  g.s_w = s_w;
-  g.bias = bias;
-  g.Y = Y;
-  g.x_rows = mx::plan_rows(T, k, E);
-  g.M = g.x_rows;
-  g.N = N;
-  g.K = K;
-  g.inv_b = 1.0f / static_cast<float>(b);
-  g.chunks = mx::scale_chunks(K, fmt);
-  g.w_blocks = (N + mx::kRowBlock - 1) / mx::kRowBlock;
-  g.experts = E;
-  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, plan, &pl, T,
-                                   static_cast<cudaStream_t>(stream)));
+  const uint8_t* p = static_cast<const uint8_t*>(plan);
+  a.X = X;
+  a.M = a.rows = mx::plan_rows(T, k, E);
+  a.K = K;
+  a.ld = ldx;
+  a.b = 1;
+  a.act = act;
+  a.codes = codes;
+  a.scales = scales;
+  a.row_scale = row_scale;
+  a.tiles = reinterpret_cast<const mx::RowTile*>(p + pl.tiles128_off);
+  a.tile_count = reinterpret_cast<const int32_t*>(p + pl.counts_off);
+  return from_cuda(mx::launch_quantize(a, dtype, fmt, static_cast<cudaStream_t>(stream)));
 }
 
 clq_status clq_mx_combine(const void* Y, clq_dtype dtype, const int32_t* rows,

@@ -1,0 +1,121 @@
+// E2M1 codes, block scales and activations on the device, shared by the quantization and
+// the product's epilogue.
+#pragma once
+
+#include "clq_device.cuh"
+
+namespace clq {
+namespace mx {
+
+// Eight values -> eight E2M1 codes, value 0 in the low nibble; nearest, ties to
+// even, saturating.
+__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r)
+      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  return r;
+}
+
+// The values of the two codes in the low byte of w (the low nibble's first).
+__device__ __forceinline__ __half2 e2m1_pair(uint32_t w) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 a, b;\n\t"
+      "mov.b16 {a, b}, %1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t}"
+      : "=r"(h)
+      : "h"(static_cast<uint16_t>(w)));
+  return *reinterpret_cast<const __half2*>(&h);
+}
+
+__device__ __forceinline__ uint32_t e4m3_byte(float v) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(v));
+  return r & 0xFFu;
+}
+
+// Value of an E4M3 byte, exact.
+__device__ __forceinline__ float e4m3_value(uint32_t byte) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(byte)));
+  return __half2float(__ushort_as_half(static_cast<uint16_t>(h)));
+}
+
+// Scale of a block whose largest absolute value has the bits amax: the exponent byte of
+// 2^ceil(log2(amax / 6)), 255 for an infinity or a NaN.
+__device__ __forceinline__ uint32_t e8m0_byte(uint32_t amax) {
+  const int e = static_cast<int>(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  return amax >= 0x7F800000u ? 255u : static_cast<uint32_t>(max(e, 0));
+}
+// 2^(127 - byte) for the bytes 0 .. 253 (of no use for 255).
+__device__ __forceinline__ float e8m0_inverse(uint32_t byte) {
+  return __uint_as_float((254u - byte) << 23);
+}
+
+// 2^(byte - 127), NaN for 255: only 0 and 255 have a mantissa bit.
+__device__ __forceinline__ float e8m0_value(uint32_t byte) {
+  return __uint_as_float((byte << 23) | (((byte + 1u) & 0xFEu) == 0u ? 0x400000u : 0u));
+}
+
+// The same to about 2^-21 of the result (of |x| for gelu), for the product's epilogue, where
+// the exact forms' 28 and 40 instructions a value took twice the tile's MMAs (65536 rows, 2048
+// channels of K = 2048: 232 us, with these 110): a code differs where a value lies that near
+// to the middle of two.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float swiglu_fast(float g, float u) {
+  return g * rcp_fast(1.f + exp2_fast(-kLog2e * g)) * u;
+}
+// erf by the rational approximation 7.1.26 of Abramowitz and Stegun, within 1.5e-7.
+__device__ __forceinline__ float gelu_fast(float x) {
+  const float z = fabsf(x) * 0.70710678118654752f;
+  const float t = rcp_fast(fmaf(0.3275911f, z, 1.f));
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f) * t;
+  const float e = p * exp2_fast(-kLog2e * z * z);  // 1 - erf(z)
+  return 0.5f * (x < 0.f ? x * e : x * (2.f - e));
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack8(const uint4& p, float* v) {
+  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = Num<T>::to_f(static_cast<uint16_t>(w[i]));
+    v[2 * i + 1] = Num<T>::to_f(static_cast<uint16_t>(w[i] >> 16));
+  }
+}
+
+// Largest absolute value, a NaN if one of them is.
+__device__ __forceinline__ float absmax3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// The activations, each operation rounded by itself.
+__device__ __forceinline__ float gelu(float x) {
+  return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.f, erff(__fmul_rn(x, 0.70710678118654752f))));
+}
+__device__ __forceinline__ float swiglu(float g, float u) {
+  return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.f, expf(-g))), u);
+}
+
+}  // namespace mx
+}  // namespace clq

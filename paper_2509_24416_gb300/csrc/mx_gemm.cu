@@ -47,7 +47,7 @@ cudaError_t launch_gemm(const uint8_t* Xq, const uint8_t* Xs, const uint8_t* Wq,
       !scales_map(&m.SW, Ws, static_cast<int64_t>(g.experts) * g.w_blocks * g.chunks, sc) ||
       !scales_map(&m.SX, Xs, blocks * g.chunks, sc))
     return cudaErrorInvalidValue;
-  const int use_tma_store = g.N % 8 == 0 ? 1 : 0;
+  const int use_tma_store = g.Yq == nullptr && g.N % 8 == 0 ? 1 : 0;
   if (use_tma_store) {
     if (!encode_tma_out_tile(&m.Y, g.Y, g.x_rows, g.N)) return cudaErrorInvalidValue;
   } else {

@@ -18,6 +18,7 @@
 #pragma once
 
 #include "gemm_common.cuh"
+#include "mx_device.cuh"
 #include "mx_kernels.h"
 
 namespace clq {
@@ -46,7 +47,7 @@ struct Cfg {
   static constexpr uint32_t TX = CG * STAGE;
   static constexpr int PARTS = NT >= 64 ? 2 : 1;  // column shares (four warps each)
   static constexpr int NCOL = NT / PARTS;
-  static constexpr int FIXED = EPI_WARPS * (EPI_BYTES + NCOL * 4);
+  static constexpr int FIXED = EPI_WARPS * 2 * EPI_BYTES;  // two staging buffers a warp
   static constexpr int S0 = (222 * 1024 - FIXED) / STAGE;
   static constexpr int S = S0 > MAX_STAGES ? MAX_STAGES : S0;
   static constexpr int OFF_A = 0;
@@ -54,8 +55,7 @@ struct Cfg {
   static constexpr int OFF_SA = OFF_B + S * B;
   static constexpr int OFF_SB = OFF_SA + S * SA;
   static constexpr int OFF_EPI = OFF_SB + S * SB;
-  static constexpr int OFF_COL = OFF_EPI + EPI_WARPS * EPI_BYTES;
-  static constexpr int BYTES = OFF_COL + EPI_WARPS * NCOL * 4;
+  static constexpr int BYTES = OFF_EPI + EPI_WARPS * 2 * EPI_BYTES;
   // Tensor memory: two accumulators of NT columns, two buffers of scales.
   static constexpr int SFA = 4 * SC;
   static constexpr int SFB = 4 * SC * XB;
@@ -140,6 +140,26 @@ struct Tile {
   int n0, row0, rows, expert;
 };
 
+__device__ __forceinline__ uint4 select(bool c, const uint4& a, const uint4& b) {
+  return make_uint4(c ? a.x : b.x, c ? a.y : b.y, c ? a.z : b.z, c ? a.w : b.w);
+}
+
+// Barrier of two warps.
+__device__ __forceinline__ void pair_barrier(int id) {
+  asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+}
+
+// Scale `byte` of block `blk` (of `blocks`) of a row of the codes that the epilogue makes;
+// the last block's warp also zeroes the bytes behind it.
+__device__ __forceinline__ void store_scale(const GemmArgs& g, int row, int blk, int blocks,
+                                            uint32_t byte) {
+  uint8_t* s = g.Ys + (static_cast<size_t>(row / kRowBlock) * g.y_chunks + (blk >> 2)) * 512 +
+               (row & 31) * 16 + ((row >> 5) & 3) * 4;
+  s[blk & 3] = static_cast<uint8_t>(byte);
+  if (blk == blocks - 1)
+    for (int q = (blk & 3) + 1; q < 4; ++q) s[q] = 0;
+}
+
 template <int NT, int CG, bool GROUPED>
 __device__ __forceinline__ Tile tile_at(const GemmArgs& g, int t, int tiles_n) {
   const int m = t / tiles_n;
@@ -158,7 +178,13 @@ __device__ __forceinline__ Tile tile_at(const GemmArgs& g, int t, int tiles_n) {
   return r;
 }
 
-template <typename OutT, int FMT, int NT, int CG, bool GROUPED>
+// What becomes of a tile: stored as OutT, or rounded to OutT, put through an activation and
+// quantized to codes with block scales (blocks of 32).
+constexpr int EPI_STORE = 0;
+constexpr int EPI_ACT = 1;     // CLQ_MX_ACT_NONE or _GELU: a channel a code
+constexpr int EPI_SWIGLU = 2;  // 8 channels of the gate, 8 of the up half, and so on
+
+template <typename OutT, int FMT, int NT, int CG, bool GROUPED, int EPI>
 __global__ void __launch_bounds__(THREADS, 1)
     mx_gemm_kernel(const __grid_constant__ CUtensorMap mapW,
                    const __grid_constant__ CUtensorMap mapX,
@@ -343,46 +369,65 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp < 4 || C::PARTS == 2) {
     const int quarter = warp & 3;
     const int part = warp < 4 ? 0 : 1;
-    const int ew = part * 4 + quarter;
-    uint8_t* staging = smem + C::OFF_EPI + ew * EPI_BYTES;
-    const uint32_t stage_addr = smem_addr(staging);
-    float* col = reinterpret_cast<float*>(smem + C::OFF_COL) + ew * C::NCOL;
+    uint8_t* staging = smem + C::OFF_EPI + (part * 4 + quarter) * 2 * EPI_BYTES;
     const uint32_t empty0 = CG == 2 ? cluster_addr(&bars.acc_empty[0], 0) : 0;
     const uint32_t ov0 = CG == 2 ? cluster_addr(&bars.ov_empty, 0) : 0;
     constexpr int NB = C::NCOL / EPI_COLS;  // blocks of 32 rows of X
-    int tc = 0;
-    for (int t = unit; t < tiles; t += units, ++tc) {
+    const int col0 = part * C::NCOL;        // this warp's tile columns
+    // A tile's channel data (channels 8 k + lane / 4 of a thread's fragments) and row
+    // scales (row 32 j + lane of the warp's columns), loaded a tile ahead.
+    float next_w[4], next_b[4], next_x[NB];
+    auto load_scales = [&](int t) {
+      if (t >= tiles) return;
       const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
-      const int n0 = T.n0 + rank * TN + quarter * 32;  // this warp's channels
-      const int col0 = part * C::NCOL;                 // and tile columns
-      const int buf = tc & 1;
-      // channels 8 k + lane / 4 of a thread's fragments; row scales of the warp's columns
-      float sw[4], bi[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int n = n0 + 8 * k + (lane >> 2);
+        const int n = T.n0 + rank * TN + quarter * 32 + 8 * k + (lane >> 2);
         const bool in = n < g.N;
         const size_t at = static_cast<size_t>(T.expert) * g.N + n;
-        sw[k] = g.inv_b;
-        if (FMT == CLQ_MX_BLOCK16) sw[k] = in ? __ldg(g.s_w + at) * g.inv_b : 0.f;
-        bi[k] = in && g.bias != nullptr
-                    ? Num<OutT>::to_f(__ldg(static_cast<const uint16_t*>(g.bias) + at))
-                    : 0.f;
+        next_w[k] = FMT == CLQ_MX_BLOCK16 ? (in ? __ldg(g.s_w + at) : 0.f) : 1.f;
+        next_b[k] = in && g.bias != nullptr
+                        ? Num<OutT>::to_f(__ldg(static_cast<const uint16_t*>(g.bias) + at))
+                        : 0.f;
       }
       if (FMT == CLQ_MX_BLOCK16) {
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
           const int i = col0 + 32 * j + lane;
-          col[32 * j + lane] = i < T.rows ? __ldg(g.s_x + T.row0 + i) : 0.f;
+          next_x[j] = i < T.rows ? __ldg(g.s_x + T.row0 + i) : 0.f;
         }
-        __syncwarp();
       }
+    };
+    load_scales(unit);
+    int tc = 0, turn = 0;
+    for (int t = unit; t < tiles; t += units, ++tc) {
+      const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
+      const int n0 = T.n0 + rank * TN + quarter * 32;  // this warp's channels
+      const int buf = tc & 1;
+      float sw[4], bi[4], sx[NB];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        sw[k] = next_w[k] * g.inv_b;
+        bi[k] = next_b[k];
+      }
+#pragma unroll
+      for (int j = 0; j < NB; ++j) sx[j] = FMT == CLQ_MX_BLOCK16 ? next_x[j] : 1.f;
+      load_scales(t + units);
       bool ok = mbar_wait_bounded(&bars.acc_full[buf], (tc >> 1) & 1, abort, g.status,
                                   kWaitLimitNs);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      auto arrive = [&](uint64_t* bar, uint32_t remote) {
+      const uint32_t lane_base =
+          tmem + buf * (NT - C::OV) + (static_cast<uint32_t>(quarter * 32) << 16);
+      const int live = n0 < g.N ? max(0, min(NB, (T.rows - col0 + 31) / 32)) : 0;
+      // Two blocks at a time leave tensor memory, and the accumulator goes back as soon as
+      // the last ones have, before they are scaled or stored.  The columns that the two
+      // accumulators share are the first buffer's last and the other's first: the warps that
+      // hold them begin there and release them by themselves.
+      const bool shares = C::OV > 0 && part == (buf == 0 ? 1 : 0);
+      const bool down = shares && buf == 0;
+      auto release = [&](uint64_t* bar, uint32_t remote) {
         tc_fence_before();
         __syncwarp();
         if (elect_one()) {
@@ -392,63 +437,143 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_arrive(bar);
         }
       };
-      // The columns that the other accumulator overlaps are the first ones of the second
-      // accumulator and the last ones of the first: they are taken out first.
-      const bool down = C::OV > 0 && buf == 0;
-      const bool guards = C::OV > 0 && part == (buf == 0 ? 1 : 0);
-      const uint32_t lane_base =
-          tmem + buf * (NT - C::OV) + (static_cast<uint32_t>(quarter * 32) << 16);
-      const int live = n0 < g.N ? max(0, min(NB, (T.rows - col0 + 31) / 32)) : 0;
-#pragma unroll 1
-      for (int j = 0; j < NB; ++j) {
-        const int blk = down ? NB - 1 - j : j;
-        if (blk < live) {
-          const int c = col0 + blk * EPI_COLS;
-          uint32_t r[2][16];  // channels 0 .. 15 and 16 .. 31
-          gemm::tmem_ld_frag(lane_base + c, r[0]);
-          gemm::tmem_ld_frag(lane_base + (16u << 16) + c, r[1]);
-          float2 sx[4];
+      constexpr int STEP = NB >= 2 ? 2 : 1;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            sx[q] = FMT == CLQ_MX_BLOCK16 ? *reinterpret_cast<const float2*>(
-                                                col + blk * 32 + 8 * q + 2 * (lane & 3))
-                                          : make_float2(1.f, 1.f);
-          gemm::tmem_ld_wait_tie(r[0]);
-          gemm::tmem_ld_wait_tie(r[1]);
-          if (use_tma_store && elect_one()) gemm::bulk_wait_read<0>();
+      for (int j0 = 0; j0 < NB; j0 += STEP) {
+        uint32_t r[STEP][2][16];  // channels 0 .. 15 and 16 .. 31 of a block
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+          const int blk = down ? NB - 1 - j0 - i : j0 + i;
+          if (blk < live) {
+            const uint32_t at = lane_base + col0 + blk * EPI_COLS;
+            gemm::tmem_ld_frag(at, r[i][0]);
+            gemm::tmem_ld_frag(at + (16u << 16), r[i][1]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+          gemm::tmem_ld_wait_tie(r[i][0]);
+          gemm::tmem_ld_wait_tie(r[i][1]);
+        }
+        if (C::OV > 0 && shares && 32 * j0 < C::OV && C::OV <= 32 * (j0 + STEP))
+          release(&bars.ov_empty, ov0);
+        if (j0 + STEP == NB) release(&bars.acc_empty[buf], empty0 + 8u * buf);
+#pragma unroll
+        for (int i = 0; i < STEP; ++i) {
+          const int blk = down ? NB - 1 - j0 - i : j0 + i;
+          if (blk >= live) continue;
+          const float sxv = down ? sx[NB - 1 - j0 - i] : sx[j0 + i];
+          uint8_t* stage = staging + turn * EPI_BYTES;
+          const uint32_t stage_addr = smem_addr(stage);
+          // the store before last has read this buffer
+          if (EPI == EPI_STORE && use_tma_store && elect_one()) gemm::bulk_wait_read<1>();
           __syncwarp();
 #pragma unroll
           for (int q = 0; q < 4; ++q) {  // rows 8 q + 2 (lane % 4), + 1
+            float2 x2 = make_float2(1.f, 1.f);
+            if (FMT == CLQ_MX_BLOCK16)
+              x2 = make_float2(__shfl_sync(0xffffffffu, sxv, 8 * q + 2 * (lane & 3)),
+                               __shfl_sync(0xffffffffu, sxv, 8 * q + 2 * (lane & 3) + 1));
             uint32_t o[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float2 acc = make_float2(__uint_as_float(r[k >> 1][4 * q + 2 * (k & 1)]),
-                                             __uint_as_float(r[k >> 1][4 * q + 2 * (k & 1) + 1]));
-              const float2 s2 = __fmul2_rn(make_float2(sw[k], sw[k]), sx[q]);
+              const float2 acc =
+                  make_float2(__uint_as_float(r[i][k >> 1][4 * q + 2 * (k & 1)]),
+                              __uint_as_float(r[i][k >> 1][4 * q + 2 * (k & 1) + 1]));
+              float2 s2 = make_float2(sw[k], sw[k]);
+              if (FMT == CLQ_MX_BLOCK16) s2 = __fmul2_rn(s2, x2);
               const float2 v = __ffma2_rn(acc, s2, make_float2(bi[k], bi[k]));
               o[k] = Num<OutT>::pack2(v.x, v.y);
             }
             stmatrix4_trans(stage_addr + gemm::staged_chunk(8 * q + (lane & 7), lane >> 3), o);
           }
-          if (use_tma_store) {
-            fence_proxy_async_smem();
+          const int row = T.row0 + col0 + 32 * blk, rows = T.rows - col0 - 32 * blk;
+          if constexpr (EPI == EPI_STORE) {
+            if (use_tma_store) {
+              fence_proxy_async_smem();
+              __syncwarp();
+              if (elect_one()) {
+                gemm::tma_store_2d(&mapY, stage, n0, row);
+                gemm::bulk_commit();
+              }
+            } else {
+              __syncwarp();
+              gemm::store_block_direct(stage_addr, lane, row, row + rows, n0, g.N,
+                                       static_cast<uint16_t*>(g.Y));
+            }
+          } else if constexpr (EPI == EPI_ACT) {
             __syncwarp();
-            if (elect_one()) {
-              gemm::tma_store_2d(&mapY, staging, n0, T.row0 + c);
-              gemm::bulk_commit();
+            // a lane a row: its 32 channels are one block
+            float v[32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              unpack8<OutT>(*reinterpret_cast<const uint4*>(stage + gemm::staged_chunk(lane, c)),
+                            v + 8 * c);
+            if (g.act == CLQ_MX_ACT_GELU) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = gelu_fast(v[i]);
+            }
+            float most = fabsf(v[0]);
+#pragma unroll
+            for (int i = 1; i < 31; i += 2) most = absmax3(most, v[i], v[i + 1]);
+            most = absmax3(most, v[31], v[31]);
+            const uint32_t byte = e8m0_byte(__float_as_uint(most));
+            const float inv = e8m0_inverse(byte);
+            uint32_t code[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[8 * c + i] = __fmul_rn(v[8 * c + i], inv);
+              code[c] = byte == 255u ? 0u : e2m1x8(v + 8 * c);
+            }
+            if (lane < rows) {
+              *reinterpret_cast<uint4*>(g.Yq + static_cast<size_t>(row + lane) * (g.N / 2) + n0 / 2) =
+                  make_uint4(code[0], code[1], code[2], code[3]);
+              store_scale(g, row + lane, n0 / 32, g.N / 32, byte);
             }
           } else {
-            __syncwarp();
-            gemm::store_block_direct(stage_addr, lane, T.row0 + c, T.row0 + T.rows, n0, g.N,
-                                     static_cast<uint16_t*>(g.Y));
-            __syncwarp();
+            // Two warps hold a block of 32 (64 channels).  Both have staged their half; each
+            // then works on half of the rows, two lanes a row.  One barrier a block: the
+            // buffers alternate.
+            pair_barrier(1 + part * 2 + (quarter >> 1));
+            const int half = lane & 1, m = 16 * (quarter & 1) + (lane >> 1);
+            const uint8_t* from = smem + C::OFF_EPI +
+                                  (part * 4 + (quarter & 2) + half) * 2 * EPI_BYTES + turn * EPI_BYTES;
+            uint4 p[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)  // the two lanes' chunks on different banks
+              p[c] = *reinterpret_cast<const uint4*>(from + gemm::staged_chunk(m, c ^ (2 * half)));
+            float v[16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float gate[8], up[8];
+              unpack8<OutT>(select(half, p[(2 * h) ^ 2], p[2 * h]), gate);
+              unpack8<OutT>(select(half, p[(2 * h + 1) ^ 2], p[2 * h + 1]), up);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[8 * h + i] = swiglu_fast(gate[i], up[i]);
+            }
+            float most = fabsf(v[0]);
+#pragma unroll
+            for (int i = 1; i < 15; i += 2) most = absmax3(most, v[i], v[i + 1]);
+            most = absmax3(most, v[15], __shfl_xor_sync(0xffffffffu, absmax3(most, v[15], v[15]), 1));
+            const uint32_t byte = e8m0_byte(__float_as_uint(most));
+            const float inv = e8m0_inverse(byte);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(v[i], inv);
+            uint2 code = make_uint2(e2m1x8(v), e2m1x8(v + 8));
+            if (byte == 255u) code = make_uint2(0, 0);
+            if (m < rows) {
+              const int f0 = (T.n0 + rank * TN + (quarter & 2) * 32) / 2;  // the block's first code
+              *reinterpret_cast<uint2*>(g.Yq + static_cast<size_t>(row + m) * (g.N / 4) + f0 / 2 +
+                                        8 * half) = code;
+              if (half == 0) store_scale(g, row + m, f0 / 32, g.N / 64, byte);
+            }
           }
+          turn ^= 1;
         }
-        if (C::OV > 0 && guards && j == C::OV / 32 - 1) arrive(&bars.ov_empty, ov0);
       }
-      arrive(&bars.acc_empty[buf], empty0 + 8u * buf);
     }
-    if (elect_one()) gemm::bulk_wait_all();
+    if (EPI == EPI_STORE && elect_one()) gemm::bulk_wait_all();
     __syncwarp();
   }
   tc_fence_before();
@@ -466,11 +591,11 @@ struct GemmMaps {
   CUtensorMap W, X, SW, SX, Y;
 };
 
-template <typename OutT, int FMT, int NT, int CG, bool GROUPED>
+template <typename OutT, int FMT, int NT, int CG, bool GROUPED, int EPI>
 cudaError_t launch_gemm_t(const GemmMaps& m, const GemmArgs& g, int use_tma_store, int grid,
                           cudaStream_t st) {
   using C = Cfg<FMT, NT, CG>;
-  auto k = mx_gemm_kernel<OutT, FMT, NT, CG, GROUPED>;
+  auto k = mx_gemm_kernel<OutT, FMT, NT, CG, GROUPED, EPI>;
   constexpr size_t smem = C::BYTES + 1024;
   cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, THREADS, nullptr);
   if (e != cudaSuccess) return e;
@@ -478,20 +603,30 @@ cudaError_t launch_gemm_t(const GemmMaps& m, const GemmArgs& g, int use_tma_stor
                             use_tma_store);
 }
 
-// The tile of nt rows (cg CTAs): instantiated for each output type and format in
-// mx_gemm_*.cu.
+// The tile of nt rows: instantiated for each output type and format in mx_gemm_*.cu.  The
+// epilogues that quantize go with the experts' products of blocks of 32.
+template <typename OutT, int FMT, int NT, int CG>
+cudaError_t launch_gemm_tile(const GemmMaps& m, const GemmArgs& g, bool grouped, int use_tma_store,
+                             int grid, cudaStream_t st) {
+  if constexpr (FMT == CLQ_MX_BLOCK32) {
+    if (g.Yq != nullptr)
+      return g.act == CLQ_MX_ACT_SWIGLU
+                 ? launch_gemm_t<OutT, FMT, NT, CG, true, EPI_SWIGLU>(m, g, 0, grid, st)
+                 : launch_gemm_t<OutT, FMT, NT, CG, true, EPI_ACT>(m, g, 0, grid, st);
+  }
+  return grouped
+             ? launch_gemm_t<OutT, FMT, NT, CG, true, EPI_STORE>(m, g, use_tma_store, grid, st)
+             : launch_gemm_t<OutT, FMT, NT, CG, false, EPI_STORE>(m, g, use_tma_store, grid, st);
+}
+
 template <typename OutT, int FMT>
 cudaError_t launch_gemm_tiles(const GemmMaps& m, const GemmArgs& g, int nt, bool grouped,
                               int use_tma_store, int grid, cudaStream_t st) {
-#define CLQ_MX_GO(NT, CG)                                                               \
-  return grouped ? launch_gemm_t<OutT, FMT, NT, CG, true>(m, g, use_tma_store, grid, st) \
-                 : launch_gemm_t<OutT, FMT, NT, CG, false>(m, g, use_tma_store, grid, st)
   switch (nt) {
-    case 32: CLQ_MX_GO(32, 1);
-    case 128: CLQ_MX_GO(128, 1);
-    default: CLQ_MX_GO(256, 2);
+    case 32: return launch_gemm_tile<OutT, FMT, 32, 1>(m, g, grouped, use_tma_store, grid, st);
+    case 128: return launch_gemm_tile<OutT, FMT, 128, 1>(m, g, grouped, use_tma_store, grid, st);
+    default: return launch_gemm_tile<OutT, FMT, 256, 2>(m, g, grouped, use_tma_store, grid, st);
   }
-#undef CLQ_MX_GO
 }
 
 using GemmFn = cudaError_t (*)(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);

@@ -30,6 +30,8 @@ struct QuantArgs {
   float* row_scale;         // BLOCK16
   const int32_t* out_rows;  // [M][k] or null
   int32_t k, rows;
+  const struct RowTile* tiles;  // X holds the rows of a plan: its tiles of 128 rows, or null
+  const int32_t* tile_count;
   int32_t* status;
 };
 cudaError_t launch_quantize(const QuantArgs& a, int dtype, int fmt, cudaStream_t st);
@@ -67,6 +69,9 @@ struct GemmArgs {
   int32_t max_tiles;  // grouped: host bound of the list
   int32_t experts;    // weight matrices (1: dense)
   int32_t x_rows;     // rows of the X code array
+  uint8_t* Yq;        // output as codes (act of the rounded product), or null
+  uint8_t* Ys;
+  int32_t act, y_chunks;
   int32_t* status;
 };
 cudaError_t launch_gemm(const uint8_t* Xq, const uint8_t* Xs, const uint8_t* Wq,

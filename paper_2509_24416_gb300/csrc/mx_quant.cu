@@ -1,5 +1,5 @@
 // Rows -> E2M1 codes with block scales, and back.
-#include "clq_device.cuh"
+#include "mx_device.cuh"
 #include "mx_kernels.h"
 
 namespace clq {
@@ -7,75 +7,6 @@ namespace mx {
 namespace {
 
 constexpr int U = 16;  // values a thread holds: half a block of 32, or one of 16
-
-// Eight values -> eight E2M1 codes, value 0 in the low nibble; nearest, ties to
-// even, saturating.
-__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
-  uint32_t r;
-  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-      "mov.b32 %0, {a, b, c, d};\n\t}"
-      : "=r"(r)
-      : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-  return r;
-}
-
-// The values of the two codes in the low byte of w (the low nibble's first).
-__device__ __forceinline__ __half2 e2m1_pair(uint32_t w) {
-  uint32_t h;
-  asm("{\n\t.reg .b8 a, b;\n\t"
-      "mov.b16 {a, b}, %1;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t}"
-      : "=r"(h)
-      : "h"(static_cast<uint16_t>(w)));
-  return *reinterpret_cast<const __half2*>(&h);
-}
-
-__device__ __forceinline__ uint32_t e4m3_byte(float v) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.f), "f"(v));
-  return r & 0xFFu;
-}
-
-// Value of a non-negative E4M3 byte below 0x7F, exact.
-__device__ __forceinline__ float e4m3_value(uint32_t byte) {
-  const uint32_t e = byte >> 3, m = byte & 7u;
-  return e == 0 ? static_cast<float>(m) * 0x1p-9f
-                : __uint_as_float(((e + 120u) << 23) | (m << 20));
-}
-
-__device__ __forceinline__ float e8m0_value(uint32_t byte) {
-  return byte == 0 ? 0x1p-127f : byte == 255 ? __uint_as_float(0x7FC00000u)
-                                             : __uint_as_float(byte << 23);
-}
-
-template <typename T>
-__device__ __forceinline__ void unpack8(const uint4& p, float* v) {
-  const uint32_t w[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = Num<T>::to_f(static_cast<uint16_t>(w[i]));
-    v[2 * i + 1] = Num<T>::to_f(static_cast<uint16_t>(w[i] >> 16));
-  }
-}
-
-// Largest absolute value, a NaN if one of them is.
-__device__ __forceinline__ float absmax3(float a, float b, float c) {
-  float r;
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
-// The activations, each operation rounded by itself.
-__device__ __forceinline__ float gelu(float x) {
-  return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.f, erff(__fmul_rn(x, 0.70710678118654752f))));
-}
-__device__ __forceinline__ float swiglu(float g, float u) {
-  return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.f, expf(-g))), u);
-}
 
 // A row's values as they are staged for the swap: the input's own 16 bits, or fp32 behind
 // an activation.
@@ -141,9 +72,17 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
     }
   }
   const int step = gridDim.x * blockDim.y;
+  // rows of a plan: whole blocks of 128, each with its first rows in use
+  const int M = a.tiles == nullptr ? a.M : min(a.M, __ldg(a.tile_count) * kRowBlock);
+  auto used = [&](int row) {
+    return row < M && (a.tiles == nullptr ||
+                       (row & (kRowBlock - 1)) < __ldg(&a.tiles[row / kRowBlock].rows));
+  };
   uint4 raw[NV];
+  bool next = false;
   auto fetch = [&](int row) {
-    if (on && row < a.M) {
+    next = on && used(row);
+    if (next) {
       const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.X) +
                                                       static_cast<size_t>(row) * a.ld) +
                        static_cast<size_t>(x) * NV;
@@ -156,9 +95,9 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
   };
   fetch(blockIdx.x * blockDim.y + y);
   int turn = 0, slot = 0;
-  for (int r0 = blockIdx.x * blockDim.y; r0 < a.M; r0 += step, turn ^= 1) {
+  for (int r0 = blockIdx.x * blockDim.y; r0 < M; r0 += step, turn ^= 1) {
     const int row = r0 + y;
-    const bool live = on && row < a.M;
+    const bool live = next;
     float v[U];
     if constexpr (ACT == CLQ_MX_ACT_SWIGLU) {
 #pragma unroll
@@ -247,10 +186,9 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
     bool bad;
     if (FMT == CLQ_MX_BLOCK32) {
       amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-      const int e = static_cast<int>(amax >> 23) - 2 + ((amax & 0x7FFFFFu) > 0x400000u ? 1 : 0);
       bad = amax >= 0x7F800000u;
-      byte = bad ? 255u : static_cast<uint32_t>(max(e, 0));
-      inv = __uint_as_float((254u - byte) << 23);
+      byte = e8m0_byte(amax);
+      inv = e8m0_inverse(byte);
     } else {
       const uint32_t wmax = __reduce_max_sync(0xffffffffu, amax);
       if (lane == 0 && wmax != 0) atomicMax(&row_max[slot][y], wmax);
@@ -381,7 +319,9 @@ cudaError_t quantize_t(const QuantArgs& a, cudaStream_t st) {
 template <typename T, int FMT>
 cudaError_t dequantize_t(const uint8_t* codes, const uint8_t* scales, const float* row_scale,
                          int M, int K, void* out, cudaStream_t st) {
-  const int tx = std::min(256, (K / 8 + 31) / 32 * 32);
+  // the fewest turns of up to 256 threads, evenly long
+  const int turns = (K / 8 + 255) / 256;
+  const int tx = ((K / 8 + turns - 1) / turns + 31) / 32 * 32;
   const int ty = 256 / tx;
   const int grid = std::min((M + ty - 1) / ty, 8 * sm_count());
   return launch_rows(dequantize_kernel<T, FMT>, grid, tx, ty, 0, st, codes, scales, row_scale, M, K,

@@ -34,6 +34,8 @@ _SIGS = {
     "clq_mx_plan_bytes": (_Z, [_I, _I, _I]),
     "clq_mx_plan": (_I, [_P, _I, _I, _I, _P, _P, _Z, _P]),
     "clq_mx_grouped_linear": (_I, [_P] * 8 + [_I] * 8 + [_P, _P]),
+    "clq_mx_grouped_linear_act": (_I, [_P] * 6 + [_I] * 8 + [_P, _P, _P]),
+    "clq_mx_quantize_rows": (_I, [_P, _I, _P] + [_I] * 7 + [_P, _P, _P, _P]),
     "clq_mx_combine": (_I, [_P, _I, _P, _P, _I, _I, _I, _I, _P, _P]),
 }
 EXPORTS = tuple(_SIGS)
@@ -93,6 +95,18 @@ def clq_mx_grouped_linear(Xq, Xs, s_x, plan, Wq, Ws, s_w, bias, T, k, E, N, K, b
                           stream):
     return load().clq_mx_grouped_linear(Xq, Xs, s_x, plan, Wq, Ws, s_w, bias, T, k, E, N, K, b,
                                         fmt, dtype, Y, stream)
+
+
+def clq_mx_grouped_linear_act(Xq, Xs, plan, Wq, Ws, bias, T, k, E, N, K, b, dtype, act, Yq, Ys,
+                              stream):
+    return load().clq_mx_grouped_linear_act(Xq, Xs, plan, Wq, Ws, bias, T, k, E, N, K, b, dtype,
+                                            act, Yq, Ys, stream)
+
+
+def clq_mx_quantize_rows(X, dtype, plan, T, k, E, K, ldx, act, fmt, codes, scales, row_scale,
+                         stream):
+    return load().clq_mx_quantize_rows(X, dtype, plan, T, k, E, K, ldx, act, fmt, codes, scales,
+                                       row_scale, stream)
 
 
 def clq_mx_combine(Y, dtype, rows, weights, T, k, D, R, out, stream):
@@ -379,7 +393,8 @@ class MXExperts:
                         self.b, ACTS[self.act], w1.codes, w1.scales, w1.row_scale, self.bias1,
                         w2.codes, w2.scales, w2.row_scale, self.bias2,
                         where=("clq_mx_plan", "clq_mx_quantize", "clq_mx_grouped_linear",
-                               "clq_mx_combine"))
+                               "clq_mx_combine", "clq_mx_grouped_linear_act",
+                               "clq_mx_quantize_rows"))
             if r is not None:
                 return r
         K = _row_input(X, None, self.perm)
@@ -399,11 +414,18 @@ class MXExperts:
         _check(clq_mx_quantize(_ptr(X), dt, T, K, X.stride(0), _ptr(self.perm), self.b, 0,
                                _format(fmt), *map(_ptr, q), _ptr(rows), k, R, st),
                "clq_mx_quantize")
-        h = self._product(*q, space, self.w1, self.bias1, self.b, T, k, R, X.dtype, st)
-        a = _empty(R, self.w2.K, fmt, X.device)
-        _check(clq_mx_quantize(_ptr(h), dt, R, self.w2.K, h.stride(0), None, 1, ACTS[self.act],
-                               _format(fmt), *map(_ptr, a), None, 0, R, st), "clq_mx_quantize")
-        y = self._product(*a, space, self.w2, self.bias2, 1, T, k, R, X.dtype, st)
+        a = _empty(R, w2.K, fmt, X.device)
+        if fmt == "block32":
+            _check(clq_mx_grouped_linear_act(_ptr(q[0]), _ptr(q[1]), _ptr(space), _ptr(w1.codes),
+                                             _ptr(w1.scales), _ptr(self.bias1), T, k, self.E,
+                                             w1.rows, K, self.b, dt, ACTS[self.act], _ptr(a[0]),
+                                             _ptr(a[1]), st), "clq_mx_grouped_linear_act")
+        else:  # a row's scale needs the whole row
+            h = self._product(*q, space, w1, self.bias1, self.b, T, k, R, X.dtype, st)
+            _check(clq_mx_quantize_rows(_ptr(h), dt, _ptr(space), T, k, self.E, w2.K, h.stride(0),
+                                        ACTS[self.act], _format(fmt), *map(_ptr, a), st),
+                   "clq_mx_quantize_rows")
+        y = self._product(*a, space, w2, self.bias2, 1, T, k, R, X.dtype, st)
         _check(clq_mx_combine(_ptr(y), dt, _ptr(rows), _ptr(routing.weights), T, k,
                               self.w2.rows, R, _ptr(out), st), "clq_mx_combine")
         return out
