@@ -69,7 +69,7 @@ clq_status grouped(const uint8_t* Xq, const uint8_t* Xs, const float* s_x, const
   g.chunks = mx::scale_chunks(K, fmt);
   g.w_blocks = (N + mx::kRowBlock - 1) / mx::kRowBlock;
   g.experts = E;
-  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, plan, &pl, T,
+  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, plan, &pl, T, k,
                                    static_cast<cudaStream_t>(stream)));
 }
 
@@ -160,7 +160,7 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
   g.w_blocks = (N + mx::kRowBlock - 1) / mx::kRowBlock;
   g.experts = 1;
   g.x_rows = M;
-  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, nullptr, nullptr, M,
+  return from_cuda(mx::launch_gemm(Xq, Xs, Wq, Ws, g, fmt, dtype, nullptr, nullptr, M, 1,
                                    static_cast<cudaStream_t>(stream)));
 }
 

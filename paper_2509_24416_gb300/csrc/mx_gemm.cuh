@@ -10,7 +10,6 @@
 // Codes arrive by TMA in the 128-byte swizzle, 256 codes a row and K step; scales, 512
 // bytes for 128 rows and four blocks as they lie in memory, go through shared memory
 // into tensor memory by tcgen05.cp, which repeats them for the four groups of lanes.
-// The scales' columns alternate between K steps.
 //
 // Roles: warp 4 copies, one lane of warp 5 issues tcgen05.cp and tcgen05.mma, warps
 // 0-3 and 6-9 take a tile out of tensor memory (32 channels and half of the columns
@@ -56,17 +55,21 @@ struct Cfg {
   static constexpr int OFF_SB = OFF_SA + S * SA;
   static constexpr int OFF_EPI = OFF_SB + S * SB;
   static constexpr int BYTES = OFF_EPI + EPI_WARPS * 2 * EPI_BYTES;
-  // Tensor memory: two accumulators of NT columns, two buffers of scales.
+  // Tensor memory: two accumulators of NT columns and the scales of NSF K steps (tcgen05
+  // copies and MMAs of one thread run in the order of their issue; a second buffer beside
+  // 256-column accumulators would make them share more columns than two blocks: 32768 x 4096
+  // -> 8192 in blocks of 16 357 us, with one 327).
   static constexpr int SFA = 4 * SC;
   static constexpr int SFB = 4 * SC * XB;
   static constexpr int SF = SFA + SFB;
-  static constexpr int NEED = 2 * NT + 2 * SF;
+  static constexpr int NSF = NT == 256 ? 1 : 2;
+  static constexpr int NEED = 2 * NT + NSF * SF;
   static constexpr int TMEM = NEED <= 128 ? 128 : NEED <= 256 ? 256 : 512;
   // Two accumulators of 256 columns and the scales do not fit: the second then starts
   // OV columns inside the first, and a tile's MMAs wait for those alone.
   static constexpr int OV = NEED > 512 ? (NEED - 512 + 31) / 32 * 32 : 0;
   static constexpr int OFF_SF = 2 * NT - OV;
-  static_assert(OFF_SF + 2 * SF <= TMEM && OV <= NCOL, "tensor memory");
+  static_assert(OFF_SF + NSF * SF <= TMEM && OV <= NCOL, "tensor memory");
   static_assert(S >= 3 && STAGE % 1024 == 0, "stages");
 };
 
@@ -237,12 +240,30 @@ __global__ void __launch_bounds__(THREADS, 1)
   // in 10^4 to 10^5 launches), so both have allocated first.
   if (warp == WARP_MMA) tmem_relinquish<CG>();
   const uint32_t tmem = bars.tmem_slot;
+  const int nk = (g.K + KC - 1) / KC;
+  const int tiles_n = (g.N + TN * CG - 1) / (TN * CG);
+  // While the previous kernel finishes, this CTA's first weights are on their way into L2:
+  // few rows meet many experts' weights, whose bytes are the work (8 tokens through 6 of 64
+  // experts: 30.1 us, with these 27.3; a dense layer's weights are often in L2 already, and
+  // the hints cost 1 x 4096 -> 16384 a microsecond).  Whatever the plan's list holds at
+  // this time, a hint changes no value.
+  if (GROUPED && NT <= 128 && warp == WARP_TMA) {
+    if (elect_one()) {
+      const int t = static_cast<int>(blockIdx.x);
+      const int expert =
+          min(max(g.tiles[min(t / tiles_n, g.max_tiles - 1)].expert, 0), g.experts - 1);
+      const int n0 = t % tiles_n * TN;
+      for (int kb = 0; kb < nk; ++kb) {
+        tma_prefetch_2d(&mapW, kb * 128, expert * g.N + n0);
+        tma_prefetch_2d(&mapSW, 0, (expert * g.w_blocks + n0 / kRowBlock) * g.chunks + kb * C::SC);
+      }
+    }
+    __syncwarp();
+  }
   pdl_wait();
   pdl_launch_dependents();
 
   volatile int32_t* abort = &bars.abort;
-  const int nk = (g.K + KC - 1) / KC;
-  const int tiles_n = (g.N + TN * CG - 1) / (TN * CG);
   const int tiles = (GROUPED ? __ldg(g.tile_count) : (g.M + NT - 1) / NT) * tiles_n;
   const int unit = static_cast<int>(blockIdx.x) / CG;
   const int units = static_cast<int>(gridDim.x) / CG;
@@ -351,7 +372,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
           }
           mma_commit<CG>(&bars.empty[s]);
-          sfbuf ^= 1;
+          if (C::NSF == 2) sfbuf ^= 1;
           if (++s == S) {
             s = 0;
             phase ^= 1;
@@ -603,37 +624,53 @@ cudaError_t launch_gemm_t(const GemmMaps& m, const GemmArgs& g, int use_tma_stor
                             use_tma_store);
 }
 
-// The tile of nt rows: instantiated for each output type and format in mx_gemm_*.cu.  The
-// epilogues that quantize go with the experts' products of blocks of 32.
+// A tile: `nt` rows of X by 128 cg channels.
+struct TileShape {
+  int nt, cg;
+};
+
+// Instantiated for each output type and format in mx_gemm_*.cu.  A plan's tiles have up to
+// 128 or 256 rows; the epilogues that quantize go with them in blocks of 32.
 template <typename OutT, int FMT, int NT, int CG>
-cudaError_t launch_gemm_tile(const GemmMaps& m, const GemmArgs& g, bool grouped, int use_tma_store,
-                             int grid, cudaStream_t st) {
+cudaError_t launch_grouped(const GemmMaps& m, const GemmArgs& g, int use_tma_store, int grid,
+                           cudaStream_t st) {
   if constexpr (FMT == CLQ_MX_BLOCK32) {
     if (g.Yq != nullptr)
       return g.act == CLQ_MX_ACT_SWIGLU
                  ? launch_gemm_t<OutT, FMT, NT, CG, true, EPI_SWIGLU>(m, g, 0, grid, st)
                  : launch_gemm_t<OutT, FMT, NT, CG, true, EPI_ACT>(m, g, 0, grid, st);
   }
-  return grouped
-             ? launch_gemm_t<OutT, FMT, NT, CG, true, EPI_STORE>(m, g, use_tma_store, grid, st)
-             : launch_gemm_t<OutT, FMT, NT, CG, false, EPI_STORE>(m, g, use_tma_store, grid, st);
+  return launch_gemm_t<OutT, FMT, NT, CG, true, EPI_STORE>(m, g, use_tma_store, grid, st);
 }
 
 template <typename OutT, int FMT>
-cudaError_t launch_gemm_tiles(const GemmMaps& m, const GemmArgs& g, int nt, bool grouped,
+cudaError_t launch_gemm_tiles(const GemmMaps& m, const GemmArgs& g, TileShape t, bool grouped,
                               int use_tma_store, int grid, cudaStream_t st) {
-  switch (nt) {
-    case 32: return launch_gemm_tile<OutT, FMT, 32, 1>(m, g, grouped, use_tma_store, grid, st);
-    case 128: return launch_gemm_tile<OutT, FMT, 128, 1>(m, g, grouped, use_tma_store, grid, st);
-    default: return launch_gemm_tile<OutT, FMT, 256, 2>(m, g, grouped, use_tma_store, grid, st);
+  if (grouped) {
+    if (t.nt == 32) return launch_grouped<OutT, FMT, 32, 1>(m, g, use_tma_store, grid, st);
+    if (t.nt == 128) return launch_grouped<OutT, FMT, 128, 1>(m, g, use_tma_store, grid, st);
+    return launch_grouped<OutT, FMT, 256, 2>(m, g, use_tma_store, grid, st);
   }
+#define CLQ_MX_GO(NT, CG) \
+  return launch_gemm_t<OutT, FMT, NT, CG, false, EPI_STORE>(m, g, use_tma_store, grid, st)
+  switch (t.nt) {
+    case 32: CLQ_MX_GO(32, 1);
+    case 64: CLQ_MX_GO(64, 1);
+    case 128:
+      if (t.cg == 1) CLQ_MX_GO(128, 1);
+      CLQ_MX_GO(128, 2);
+    default:
+      if (t.cg == 1) CLQ_MX_GO(256, 1);
+      CLQ_MX_GO(256, 2);
+  }
+#undef CLQ_MX_GO
 }
 
-using GemmFn = cudaError_t (*)(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
-cudaError_t gemm_block32_f16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
-cudaError_t gemm_block32_bf16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
-cudaError_t gemm_block16_f16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
-cudaError_t gemm_block16_bf16(const GemmMaps&, const GemmArgs&, int, bool, int, int, cudaStream_t);
+using GemmFn = cudaError_t (*)(const GemmMaps&, const GemmArgs&, TileShape, bool, int, int, cudaStream_t);
+cudaError_t gemm_block32_f16(const GemmMaps&, const GemmArgs&, TileShape, bool, int, int, cudaStream_t);
+cudaError_t gemm_block32_bf16(const GemmMaps&, const GemmArgs&, TileShape, bool, int, int, cudaStream_t);
+cudaError_t gemm_block16_f16(const GemmMaps&, const GemmArgs&, TileShape, bool, int, int, cudaStream_t);
+cudaError_t gemm_block16_bf16(const GemmMaps&, const GemmArgs&, TileShape, bool, int, int, cudaStream_t);
 
 }  // namespace mx
 }  // namespace clq

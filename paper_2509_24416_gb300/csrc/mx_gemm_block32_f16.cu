@@ -3,9 +3,9 @@
 
 namespace clq {
 namespace mx {
-cudaError_t gemm_block32_f16(const GemmMaps& m, const GemmArgs& g, int nt, bool grouped,
+cudaError_t gemm_block32_f16(const GemmMaps& m, const GemmArgs& g, TileShape t, bool grouped,
                             int use_tma_store, int grid, cudaStream_t st) {
-  return launch_gemm_tiles<__half, CLQ_MX_BLOCK32>(m, g, nt, grouped, use_tma_store, grid, st);
+  return launch_gemm_tiles<__half, CLQ_MX_BLOCK32>(m, g, t, grouped, use_tma_store, grid, st);
 }
 }  // namespace mx
 }  // namespace clq

@@ -30,6 +30,7 @@ struct QuantArgs {
   float* row_scale;         // BLOCK16
   const int32_t* out_rows;  // [M][k] or null
   int32_t k, rows;
+  int32_t block_rows;           // filled in by the launcher
   const struct RowTile* tiles;  // X holds the rows of a plan: its tiles of 128 rows, or null
   const int32_t* tile_count;
   int32_t* status;
@@ -76,7 +77,7 @@ struct GemmArgs {
 };
 cudaError_t launch_gemm(const uint8_t* Xq, const uint8_t* Xs, const uint8_t* Wq,
                         const uint8_t* Ws, const GemmArgs& g, int fmt, int dtype, const void* plan,
-                        const PlanLayout* pl, int T, cudaStream_t st);
+                        const PlanLayout* pl, int T, int k, cudaStream_t st);
 
 struct RouteArgs {
   const void* logits;

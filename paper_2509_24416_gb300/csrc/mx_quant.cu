@@ -7,6 +7,7 @@ namespace mx {
 namespace {
 
 constexpr int U = 16;  // values a thread holds: half a block of 32, or one of 16
+constexpr int MAX_ROWS = 256;  // rows that a block works on at a time
 
 // A row's values as they are staged for the swap: the input's own 16 bits, or fp32 behind
 // an activation.
@@ -18,6 +19,46 @@ template <typename T>
 struct Staged<T, CLQ_MX_ACT_NONE> {
   using type = uint16_t;
 };
+
+// v H_b: stages 1, 2, 4, 8 in a thread's values, 16 and up between lanes (K % b == 0, so the
+// b / 16 lanes of a block are neighbours, all on or all off).
+__device__ __forceinline__ void rotate(float (&v)[U], int b, int lane) {
+  if (b > 1) {
+#pragma unroll
+    for (int i = 0; i < U; i += 2) {
+      const float p = v[i], q = v[i + 1];
+      v[i] = __fadd_rn(p, q);
+      v[i + 1] = __fsub_rn(p, q);
+    }
+  }
+  // two values an instruction; q - p as p (-1) + q, whose product is exact
+  auto fma2 = [](float& x0, float& x1, float f, float y0, float y1) {
+    const float2 r = __ffma2_rn(make_float2(x0, x1), make_float2(f, f), make_float2(y0, y1));
+    x0 = r.x;
+    x1 = r.y;
+  };
+#pragma unroll
+  for (int h = 2; h < U; h *= 2) {
+    if (h < b) {
+#pragma unroll
+      for (int i = 0; i < U; i += 2)
+        if ((i & h) == 0) {
+          const float p0 = v[i], p1 = v[i + 1];
+          fma2(v[i], v[i + 1], 1.f, v[i + h], v[i + h + 1]);
+          fma2(v[i + h], v[i + h + 1], -1.f, p0, p1);
+        }
+    }
+  }
+  for (int m = 1; m * U < b; m *= 2) {
+    const float sign = (lane & m) ? -1.f : 1.f;
+#pragma unroll
+    for (int i = 0; i < U; i += 2) {
+      const float o0 = __shfl_xor_sync(0xffffffffu, v[i], m);
+      const float o1 = __shfl_xor_sync(0xffffffffu, v[i + 1], m);
+      fma2(v[i], v[i + 1], sign, o0, o1);
+    }
+  }
+}
 
 // Where element e of a row is staged: one word is left out after every 32, so that the
 // lanes' reads of evenly spaced elements (a swap vector ascends in each half) fall on
@@ -32,22 +73,30 @@ __host__ __device__ __forceinline__ int staged_row(int K) {
   return (staged_at<S>(K) + 7) / 8 * 8;
 }
 
-// blockDim.x threads a row (a multiple of 32; thread x holds values 16 x .. + 15),
-// blockDim.y rows at a time.  One pass over X, bound by memory: the next row's loads are
-// issued before a row is worked on, and a row costs one barrier for its swap (two staging
-// buffers in turn) and one for its largest value (three slots in turn).
+// A block works on R = a.block_rows rows at a time, thread t on values 16 x .. + 15 of row y,
+// t = y K / 16 + x (lanes of a warp may be of different rows; those that share a block of
+// the rotation or a scale are neighbours in one warp, since both divide K).  One pass over X,
+// bound by memory where nothing is applied, else by instructions and, with a swap, by shared
+// memory (a random swap's reads take 3.5 turns on the banks, the rotation's shuffles the
+// rest): the next row's loads are issued before a row is worked on, and a row costs one
+// barrier for its swap (two staging buffers in turn) and one for its largest value (three
+// slots in turn).  Two rows a thread, a staged word holding an element of both, were slower
+// (8192 x 1152 swapped 18.0 us for 17.2, 16384 x 4608 without 39.4 for 35.3: registers).
 template <typename T, int FMT, int ACT, bool SWAP>
 __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
   using S = typename Staged<T, ACT>::type;
   extern __shared__ __align__(16) uint8_t stage_raw[];  // SWAP: two rows of S for each y
-  __shared__ uint32_t row_max[3][32];
+  __shared__ uint32_t row_max[3][MAX_ROWS];
   constexpr int NV = ACT == CLQ_MX_ACT_SWIGLU ? 4 : 2;  // 16-byte loads of a thread
-  const int units = a.K / U;
-  const int x = threadIdx.x, y = threadIdx.y, lane = x & 31;
-  const bool on = x < units;
+  const int units = a.K / U, R = a.block_rows;
+  const int lane = threadIdx.x & 31;
+  const bool on = static_cast<int>(threadIdx.x) < R * units;
+  const int y = on ? threadIdx.x / units : R, x = threadIdx.x - y * units;
   const int chunks = scale_chunks(a.K, FMT);
+  // the rows that this warp's lanes are of
+  const int y0 = __shfl_sync(0xffffffffu, y, 0), y1 = __shfl_sync(0xffffffffu, y, 31);
   if (FMT == CLQ_MX_BLOCK16) {
-    if (x < 3) row_max[x][y] = 0;
+    for (int i = threadIdx.x; i < 3 * MAX_ROWS; i += blockDim.x) (&row_max[0][0])[i] = 0;
     __syncthreads();
   }
   pdl_wait();
@@ -71,7 +120,7 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       src[i / 2 + 1] = static_cast<uint32_t>(p[2] | (p[3] << 16));
     }
   }
-  const int step = gridDim.x * blockDim.y;
+  const int step = gridDim.x * R;
   // rows of a plan: whole blocks of 128, each with its first rows in use
   const int M = a.tiles == nullptr ? a.M : min(a.M, __ldg(a.tile_count) * kRowBlock);
   auto used = [&](int row) {
@@ -93,9 +142,9 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       for (int i = 0; i < NV; ++i) raw[i] = make_uint4(0, 0, 0, 0);
     }
   };
-  fetch(blockIdx.x * blockDim.y + y);
+  fetch(blockIdx.x * R + y);
   int turn = 0, slot = 0;
-  for (int r0 = blockIdx.x * blockDim.y; r0 < M; r0 += step, turn ^= 1) {
+  for (int r0 = blockIdx.x * R; r0 < M; r0 += step, turn ^= 1) {
     const int row = r0 + y;
     const bool live = next;
     float v[U];
@@ -118,7 +167,7 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
     }
     if constexpr (SWAP) {
       S* s = reinterpret_cast<S*>(stage_raw) +
-             static_cast<size_t>(turn * blockDim.y + y) * staged_row<S>(a.K);
+             static_cast<size_t>(turn * R + y) * staged_row<S>(a.K);
       if (on) {
         uint32_t* w = reinterpret_cast<uint32_t*>(s + staged_at<S>(x * U));
         if constexpr (ACT == CLQ_MX_ACT_NONE) {
@@ -149,32 +198,7 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
     } else {
       fetch(row + step);
     }
-    // H_b: stages 1, 2, 4, 8 in a thread's values, 16 and up between lanes (K % b ==
-    // 0, so the b / 16 lanes of a block are neighbours, all on or all off).
-#pragma unroll
-    for (int h = 1; h < U; h *= 2) {
-      if (h < a.b) {
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-          if ((i & h) == 0) {
-            const float p = v[i], q = v[i + h];
-            v[i] = __fadd_rn(p, q);
-            v[i + h] = __fsub_rn(p, q);
-          }
-      }
-    }
-    for (int m = 1; m * U < a.b; m *= 2) {
-      // o + v or o - v as one fused operation: the product with 1 or -1 is exact
-      const float sign = (lane & m) ? -1.f : 1.f;
-#pragma unroll
-      for (int i = 0; i < U; i += 2) {
-        const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, v[i], m),
-                                     __shfl_xor_sync(0xffffffffu, v[i + 1], m));
-        const float2 r = __ffma2_rn(make_float2(v[i], v[i + 1]), make_float2(sign, sign), o);
-        v[i] = r.x;
-        v[i + 1] = r.y;
-      }
-    }
+    rotate(v, a.b, lane);
     // Largest absolute value; from here on by its bits, a NaN's being above an infinity's.
     float most = fabsf(v[0]);
 #pragma unroll
@@ -190,13 +214,15 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       byte = e8m0_byte(amax);
       inv = e8m0_inverse(byte);
     } else {
-      const uint32_t wmax = __reduce_max_sync(0xffffffffu, amax);
-      if (lane == 0 && wmax != 0) atomicMax(&row_max[slot][y], wmax);
+      for (int r = y0; r <= min(y1, R - 1); ++r) {
+        const uint32_t wmax = __reduce_max_sync(0xffffffffu, y == r ? amax : 0u);
+        if (lane == 0 && wmax != 0) atomicMax(&row_max[slot][r], wmax);
+      }
       __syncthreads();
-      const uint32_t rmax = row_max[slot][y];
+      const uint32_t rmax = on ? row_max[slot][y] : 0u;
       slot = slot == 2 ? 0 : slot + 1;
       // used again in two rows' time, behind the next row's barrier
-      if (x == 0) row_max[slot == 2 ? 0 : slot + 1][y] = 0;
+      if (on && x == 0) row_max[slot == 2 ? 0 : slot + 1][y] = 0;
       bad = rmax >= 0x7F800000u;
       srow = bad ? __uint_as_float(0x7FC00000u)
                  : fmaxf(__fmul_rn(__uint_as_float(rmax), 1.f / 2688.f), 0x1p-100f);
@@ -211,13 +237,10 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
     }
     uint2 q = make_uint2(e2m1x8(v), e2m1x8(v + 8));
     if (bad) q = make_uint2(0, 0);
-    // Four scales a word: those of this lane and of three lanes (pairs) behind it.
-    if (!on) byte = 0;
-    constexpr int STEP = FMT == CLQ_MX_BLOCK32 ? 2 : 1;
-    uint32_t word = byte;
-#pragma unroll
-    for (int j = 1; j < 4; ++j) word |= __shfl_down_sync(0xffffffffu, byte, j * STEP) << (8 * j);
-    const bool writer = live && (lane & (4 * STEP - 1)) == 0;
+    // The scale's byte, by the block's first lane; the last block's also zeroes those behind.
+    constexpr int LANES = FMT == CLQ_MX_BLOCK32 ? 2 : 1;
+    const bool writer = x % LANES == 0;
+    const int blk = x / LANES, blocks = units / LANES;
     const int n = a.out_rows == nullptr ? 1 : a.k;
     if (live) {
       for (int j = 0; j < n; ++j) {
@@ -229,15 +252,19 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
         }
         *reinterpret_cast<uint2*>(a.codes + static_cast<size_t>(at) * (a.K / 2) + x * 8) = q;
         if (writer) {
-          const size_t c = static_cast<size_t>(at / kRowBlock) * chunks + x / (4 * STEP);
-          *reinterpret_cast<uint32_t*>(a.scales + c * 512 + (at & 31) * 16 + ((at >> 5) & 3) * 4) =
-              word;
+          uint8_t* p = a.scales + (static_cast<size_t>(at / kRowBlock) * chunks + (blk >> 2)) * 512 +
+                       (at & 31) * 16 + ((at >> 5) & 3) * 4;
+          p[blk & 3] = static_cast<uint8_t>(byte);
+          if (blk == blocks - 1)
+            for (int i = (blk & 3) + 1; i < 4; ++i) p[i] = 0;
         }
         if (FMT == CLQ_MX_BLOCK16 && x == 0) a.row_scale[at] = srow;
       }
     }
   }
 }
+
+constexpr int TURNS = 4;  // groups of eight codes that a thread takes of a row at a time
 
 // One thread eight codes of a row, so that a warp's stores are whole lines; blockDim.y rows
 // at a time.
@@ -247,30 +274,57 @@ __global__ void __launch_bounds__(256)
                       const float* __restrict__ row_scale, int M, int K, T* out) {
   const int units = K / 8;
   const int chunks = scale_chunks(K, FMT);
+  const int step = gridDim.x * blockDim.y;
   pdl_wait();
   pdl_launch_dependents();
-  for (int row = blockIdx.x * blockDim.y + threadIdx.y; row < M; row += gridDim.x * blockDim.y) {
-    const uint8_t* sc = scales + static_cast<size_t>(row / kRowBlock) * chunks * 512 +
-                        (row & 31) * 16 + ((row >> 5) & 3) * 4;
-    const float r = FMT == CLQ_MX_BLOCK32 ? 1.f : __ldg(row_scale + row);
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(codes) + static_cast<size_t>(row) * units;
-    uint4* dst = reinterpret_cast<uint4*>(out) + static_cast<size_t>(row) * units;
-#pragma unroll 4
-    for (int x = threadIdx.x; x < units; x += blockDim.x) {
-      const uint32_t w = __ldg(q + x);
-      const int blk = FMT == CLQ_MX_BLOCK32 ? x >> 2 : x >> 1;
-      const uint32_t byte = __ldg(sc + (blk >> 2) * 512 + (blk & 3));
-      const float s = FMT == CLQ_MX_BLOCK32 ? e8m0_value(byte) : e4m3_value(byte);
-      uint32_t o[4];
+  for (int x0 = threadIdx.x; x0 < units; x0 += TURNS * blockDim.x) {
+    uint32_t w[TURNS], byte[TURNS];
+    float r = 1.f;
+    // a row's loads are issued before the last one's values are stored
+    auto fetch = [&](int row) {
+      if (row >= M) return;
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(codes) + static_cast<size_t>(row) * units;
+      const uint8_t* sc = scales + static_cast<size_t>(row / kRowBlock) * chunks * 512 +
+                          (row & 31) * 16 + ((row >> 5) & 3) * 4;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        // code times block scale is exact; one rounding by the row scale, one by T
-        float2 v = __half22float2(e2m1_pair(w >> (8 * j)));
-        v = __fmul2_rn(v, make_float2(s, s));
-        if (FMT == CLQ_MX_BLOCK16) v = __fmul2_rn(v, make_float2(r, r));
-        o[j] = Num<T>::pack2(v.x, v.y);
+      for (int i = 0; i < TURNS; ++i) {
+        const int x = x0 + i * blockDim.x;
+        if (x < units) {
+          const int blk = FMT == CLQ_MX_BLOCK32 ? x >> 2 : x >> 1;
+          w[i] = __ldg(q + x);
+          byte[i] = __ldg(sc + (blk >> 2) * 512 + (blk & 3));
+        }
       }
-      dst[x] = make_uint4(o[0], o[1], o[2], o[3]);
+      if (FMT == CLQ_MX_BLOCK16) r = __ldg(row_scale + row);
+    };
+    int row = blockIdx.x * blockDim.y + threadIdx.y;
+    fetch(row);
+    for (; row < M; row += step) {
+      uint32_t now[TURNS], scale[TURNS];
+      const float rs = r;
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        now[i] = w[i];
+        scale[i] = byte[i];
+      }
+      fetch(row + step);
+      uint4* dst = reinterpret_cast<uint4*>(out) + static_cast<size_t>(row) * units;
+#pragma unroll
+      for (int i = 0; i < TURNS; ++i) {
+        const int x = x0 + i * blockDim.x;
+        if (x >= units) break;
+        const float s = FMT == CLQ_MX_BLOCK32 ? e8m0_value(scale[i]) : e4m3_value(scale[i]);
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          // code times block scale is exact; one rounding by the row scale, one by T
+          float2 v = __half22float2(e2m1_pair(now[i] >> (8 * j)));
+          v = __fmul2_rn(v, make_float2(s, s));
+          if (FMT == CLQ_MX_BLOCK16) v = __fmul2_rn(v, make_float2(rs, rs));
+          o[j] = Num<T>::pack2(v.x, v.y);
+        }
+        dst[x] = make_uint4(o[0], o[1], o[2], o[3]);
+      }
     }
   }
 }
@@ -298,22 +352,38 @@ cudaError_t launch_rows(void (*k)(KArgs...), int grid, int tx, int ty, size_t sm
 }
 
 template <typename T, int FMT>
-cudaError_t quantize_t(const QuantArgs& a, cudaStream_t st) {
-  const int tx = (a.K / U + 31) / 32 * 32;
-  const int ty = std::max(1, std::min(32, 256 / tx));
+cudaError_t quantize_t(const QuantArgs& args, cudaStream_t st) {
+  // Rows of a block: of those with up to 512 threads the number that leaves the fewest lanes
+  // idle, among equals the smallest of at least 128 threads; with few rows no more than give
+  // every SM two blocks (256 x 1152: 3.1 us with one row, 3.9 with four).
+  QuantArgs a = args;
+  const int units = a.K / U;
+  int rows = 1;
+  double best = 0;
+  const int most = std::min(MAX_ROWS, a.M / (2 * sm_count()));
+  for (int r = 1; r * units <= 512 && r <= most; ++r) {
+    const int threads = (r * units + 31) / 32 * 32;
+    const double used = static_cast<double>(r * units) / threads;
+    if (used > best + 1e-9 || r * units <= 128) {
+      best = used;
+      rows = r;
+    }
+  }
+  a.block_rows = rows;
+  const int threads = (rows * units + 31) / 32 * 32;
   const size_t smem = a.perm == nullptr ? 0
                       : a.act == CLQ_MX_ACT_NONE
-                          ? static_cast<size_t>(2 * ty) * staged_row<uint16_t>(a.K) * 2
-                          : static_cast<size_t>(2 * ty) * staged_row<float>(a.K) * 4;
+                          ? static_cast<size_t>(2 * rows) * staged_row<uint16_t>(a.K) * 2
+                          : static_cast<size_t>(2 * rows) * staged_row<float>(a.K) * 4;
   void (*k)(QuantArgs) =
       a.act == CLQ_MX_ACT_GELU     ? pick<T, FMT, CLQ_MX_ACT_GELU>(a.perm)
       : a.act == CLQ_MX_ACT_SWIGLU ? pick<T, FMT, CLQ_MX_ACT_SWIGLU>(a.perm)
                                    : pick<T, FMT, CLQ_MX_ACT_NONE>(a.perm);
   int per_sm = 0;
-  cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, tx * ty, &per_sm);
+  cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, threads, &per_sm);
   if (e != cudaSuccess) return e;
-  const int grid = std::min((a.M + ty - 1) / ty, std::max(1, per_sm) * sm_count());
-  return launch_rows(k, grid, tx, ty, smem, st, a);
+  const int grid = std::min((a.M + rows - 1) / rows, std::max(1, per_sm) * sm_count());
+  return launch_pdl(k, grid, threads, smem, st, a);
 }
 
 template <typename T, int FMT>
