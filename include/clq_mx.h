@@ -17,7 +17,8 @@
  *
  * CODES.  E2M1: sign bit 3; 0, 1, .., 7 of the other bits are 0, 0.5, 1, 1.5,
  * 2, 3, 4, 6.  A row of K codes is K / 2 bytes, code 2j in the low nibble of
- * byte j; rows are contiguous.  K % 32 == 0, 32 <= K <= 16384.
+ * byte j; rows are contiguous.  K % 32 == 0, 32 <= K <= 16384; fewer than 2^30
+ * rows.
  * SCALES.  One byte a block of `block` codes of a row:
  *   CLQ_MX_BLOCK32  blocks of 32, E8M0 bytes: 2^(byte - 127), 0xFF is NaN;
  *   CLQ_MX_BLOCK16  blocks of 16, E4M3 bytes (not negative), and an fp32
@@ -168,7 +169,8 @@ clq_status clq_mx_quantize_rows(const void* X, clq_dtype dtype, const void* plan
 
 /*
  * out[t] = sum_j weights[t][j] Y[rows[t][j]] over the places with rows >= 0, in
- * the order of j, in fp32.  Y: device [R][D] of `dtype`, D % 8 == 0; out: [T][D].
+ * the order of j, in fp32.  Y: device [R][D] of `dtype`, D % 8 == 0, D <= 2^24; out:
+ * [T][D].
  */
 clq_status clq_mx_combine(const void* Y, clq_dtype dtype, const int32_t* rows,
                           const float* weights, int32_t T, int32_t k, int32_t D, int32_t R,

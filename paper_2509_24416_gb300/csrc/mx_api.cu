@@ -14,6 +14,7 @@ using namespace clq;
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool valid_dtype(int d) { return d == CLQ_F16 || d == CLQ_BF16; }
 bool valid_format(int f) { return f == CLQ_MX_BLOCK32 || f == CLQ_MX_BLOCK16; }
+constexpr int kMaxRows = (1 << 30) - 1;  // row indices and a grid's step beyond them fit an int
 bool valid_k(int K) { return K >= 32 && K <= 16384 && K % 32 == 0; }
 bool valid_b(int b, int K) { return b >= 1 && b <= 256 && (b & (b - 1)) == 0 && K % b == 0; }
 clq_status from_cuda(cudaError_t e) { return e == cudaSuccess ? CLQ_OK : CLQ_ERR_CUDA; }
@@ -30,7 +31,7 @@ clq_status check_codes(const uint8_t* q, const uint8_t* s, const float* rows, in
 
 bool valid_routing(int T, int k, int E) {
   return T >= 0 && E >= 1 && E <= 512 && k >= 1 && k <= 32 && k <= E &&
-         static_cast<int64_t>(T) * k + 128ll * E < (1ll << 31);
+         static_cast<int64_t>(T) * k + 128ll * E <= kMaxRows;
 }
 
 // The experts' products, their output in Y or, behind `act`, as codes in Yq / Ys.
@@ -90,7 +91,7 @@ clq_status clq_mx_quantize(const void* X, clq_dtype dtype, int32_t M, int32_t K,
       act > CLQ_MX_ACT_SWIGLU || M < 0 || rows < 0 || (out_rows != nullptr && k < 1))
     return CLQ_ERR_INVALID_ARG;
   const int64_t width = act == CLQ_MX_ACT_SWIGLU ? 2ll * K : K;
-  if (!valid_k(K) || !valid_b(b, K) || ldx < width) return CLQ_ERR_SHAPE;
+  if (!valid_k(K) || !valid_b(b, K) || ldx < width || M > kMaxRows) return CLQ_ERR_SHAPE;
   if (out_rows == nullptr && rows < M) return CLQ_ERR_SHAPE;
   if (ldx % 8 != 0) return CLQ_ERR_ALIGN;
   if (M == 0) return CLQ_OK;
@@ -122,7 +123,7 @@ clq_status clq_mx_dequantize(const uint8_t* codes, const uint8_t* scales, const 
                              int32_t M, int32_t K, clq_mx_format fmt, clq_dtype dtype, void* out,
                              void* stream) {
   if (!valid_dtype(dtype) || !valid_format(fmt) || M < 0) return CLQ_ERR_INVALID_ARG;
-  if (!valid_k(K)) return CLQ_ERR_SHAPE;
+  if (!valid_k(K) || M > kMaxRows) return CLQ_ERR_SHAPE;
   if (M == 0) return CLQ_OK;
   if (out == nullptr) return CLQ_ERR_INVALID_ARG;
   if (!aligned(out, 16)) return CLQ_ERR_ALIGN;
@@ -139,7 +140,7 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
                          int32_t M, int32_t N, int32_t K, int32_t b, clq_mx_format fmt,
                          clq_dtype dtype, void* Y, void* stream) {
   if (!valid_dtype(dtype) || !valid_format(fmt) || M < 0 || N < 0) return CLQ_ERR_INVALID_ARG;
-  if (!valid_k(K) || !valid_b(b, K)) return CLQ_ERR_SHAPE;
+  if (!valid_k(K) || !valid_b(b, K) || M > kMaxRows || N > kMaxRows) return CLQ_ERR_SHAPE;
   if (M == 0 || N == 0) return CLQ_OK;
   if (Y == nullptr) return CLQ_ERR_INVALID_ARG;
   if (!aligned(Y, 16) || (bias != nullptr && !aligned(bias, 2))) return CLQ_ERR_ALIGN;
@@ -282,7 +283,7 @@ clq_status clq_mx_combine(const void* Y, clq_dtype dtype, const int32_t* rows,
                           const float* weights, int32_t T, int32_t k, int32_t D, int32_t R,
                           void* out, void* stream) {
   if (!valid_dtype(dtype) || T < 0 || k < 1 || R < 0) return CLQ_ERR_INVALID_ARG;
-  if (D < 8 || D % 8 != 0) return CLQ_ERR_SHAPE;
+  if (D < 8 || D % 8 != 0 || D > (1 << 24)) return CLQ_ERR_SHAPE;
   if (T == 0) return CLQ_OK;
   if (Y == nullptr || rows == nullptr || weights == nullptr || out == nullptr)
     return CLQ_ERR_INVALID_ARG;

@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       srow = bad ? __uint_as_float(0x7FC00000u)
                  : fmaxf(__fmul_rn(__uint_as_float(rmax), 1.f / 2688.f), 0x1p-100f);
       byte = bad ? 0u : e4m3_byte(__fdiv_rn(__uint_as_float(amax), __fmul_rn(6.f, srow)));
-      inv = byte == 0 ? 0.f : __fdiv_rn(1.f, __fmul_rn(e4m3_value(byte), srow));
+      inv = byte == 0 ? 0.f : __frcp_rn(__fmul_rn(e4m3_value(byte), srow));
     }
 #pragma unroll
     for (int i = 0; i < U; i += 2) {

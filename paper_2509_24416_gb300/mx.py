@@ -132,6 +132,13 @@ def _on(t, dtype, device, name):
         raise ValueError("%s must be a contiguous %s tensor on %s" % (name, dtype, device))
 
 
+def _on_gpu(*tensors):
+    """The C calls take addresses: what they are of is checked here."""
+    tensors = [t for t in tensors if t is not None]
+    if not all(t.is_cuda and t.device == tensors[0].device for t in tensors):
+        raise ValueError("expected tensors on one GPU, got %s" % [str(t.device) for t in tensors])
+
+
 class MXTensor:
     """Rows of E2M1 codes: ``codes`` uint8 [.., rows, K / 2], ``scales`` uint8 [.., *scale_shape]
     and, for "block16", ``row_scale`` fp32 [.., rows]; a leading dimension is a stack (of experts'
@@ -205,6 +212,7 @@ def quantize(X, fmt="block32", perm=None, b=1, act=None, stream=None):
     if r is not None:
         return MXTensor._made(*r, fmt)
     K = _row_input(X, act, perm)
+    _on_gpu(X)
     M = X.shape[0]
     codes, scales, rows = _empty(M, K, fmt, X.device)
     _check(clq_mx_quantize(_ptr(X), _dt(X), M, K, X.stride(0), _ptr(perm), b, ACTS[act], f,
@@ -224,6 +232,7 @@ def dequantize(q, dtype=torch.bfloat16, stream=None):
                     where=("clq_mx_dequantize",))
         if r is not None:
             return r
+    _on_gpu(q.codes)
     out = torch.empty((q.rows, q.K), dtype=dtype, device=q.codes.device)
     _check(clq_mx_dequantize(_ptr(q.codes), _ptr(q.scales), _ptr(q.row_scale), q.rows, q.K,
                              _format(q.fmt), _dt(out), _ptr(out), _stream(stream)),
@@ -245,6 +254,7 @@ def linear(x, w, bias=None, b=1, dtype=torch.bfloat16, Y=None, stream=None):
     if x.codes.dim() != 2 or w.codes.dim() != 2:
         raise ValueError("expected arrays of rows, got a stack")
     dev = x.codes.device
+    _on_gpu(x.codes, w.codes)
     if Y is None:
         Y = torch.empty((x.rows, w.rows), dtype=dtype, device=dev)
     else:
@@ -319,6 +329,7 @@ def route(logits, k, scoring="softmax", balance=None, groups=1, top_groups=1, gr
     _on(balance, torch.float32, logits.device, "balance")
     if balance is not None and tuple(balance.shape) != (E,):
         raise ValueError("balance must have shape (%d,)" % E)
+    _on_gpu(logits)
     experts = torch.empty((T, k), dtype=torch.int32, device=logits.device)
     weights = torch.empty((T, k), dtype=torch.float32, device=logits.device)
     dtype = CLQ_F32 if logits.dtype == torch.float32 else _dt(logits)
@@ -334,6 +345,7 @@ def plan(routing, stream=None):
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, plan, routing)
     T, k = routing.experts.shape
+    _on_gpu(routing.experts)
     nbytes = clq_mx_plan_bytes(T, k, routing.E)
     if nbytes == 0:
         raise clq.ClqError(2, "clq_mx_plan")
@@ -405,6 +417,7 @@ class MXExperts:
                                                                         routing.E))
         for bias in (self.bias1, self.bias2):
             _on(bias, X.dtype, X.device, "bias")
+        _on_gpu(X, routing.experts, routing.weights, w1.codes, w2.codes)
         out = torch.empty((T, self.w2.rows), dtype=X.dtype, device=X.device)
         if T == 0:
             return out

@@ -177,6 +177,27 @@ def test_linear_exact_codes(fmt, M):
     assert torch.equal(got.cpu(), wide.to(F16))
 
 
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K,N", [(20, 8192, 140), (70, 2048, 129), (300, 8192, 700), (600, 4096, 1100), (1500, 1152, 3456),
+                                   (4096, 2048, 1152), (8192, 512, 1304)])
+def test_linear_every_step_takes_its_own_scales(fmt, M, K, N):
+    """Scales of 1 and 2 at random over many K steps, sums that fp32 holds: exact, in every tile shape."""
+    g = gen(M + K)
+    one, two = (127, 128) if fmt == "block32" else (56, 64)
+    def tensor(rows):
+        codes = torch.randint(0, 256, (rows, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+        pick = torch.randint(0, 2, mx.scale_shape(rows, K, fmt), generator=g, device=DEV)
+        scales = (one + (two - one) * pick).to(torch.uint8)
+        return mx.MXTensor(codes, scales, torch.ones(rows, device=DEV) if fmt == "block16" else None, fmt)
+    x, w = tensor(M), tensor(N)
+    rows = torch.randperm(M, generator=g, device=DEV)[:200].cpu().numpy()  # of the result
+    want = ref.values_of(x)[rows] @ ref.values_of(w).T
+    # multiples of 1/4 below 36 K: at most 4 * 36 * 8192 < 2^24 steps
+    for _ in range(3):
+        got = mx.linear(x, w, dtype=F16)[torch.from_numpy(rows).to(DEV)]
+        assert torch.equal(got.cpu(), torch.from_numpy(want).to(torch.float32).to(F16))
+
+
 def test_linear_nan_scale_stays_in_its_row():
     X = rows_of(gen(3), 300, 256, BF16)
     X[37, 100] = float("nan")
@@ -315,7 +336,44 @@ def test_experts(T, D, F, E, k, fmt, act, bias):
     assert np.linalg.norm(y - want) <= 1e-2 * np.linalg.norm(want)
 
 
-def test_combine_and_refusals():
+@pytest.mark.parametrize("act", ["swiglu", "gelu", None])
+@pytest.mark.parametrize("T,E,F,dtype", [(5, 4, 32, BF16), (32, 60, 96, F16), (33, 3, 160, BF16), (500, 4, 544, F16),
+                                         (3000, 4, 288, BF16)])
+def test_fused_activation_is_the_separate_one(act, T, E, F, dtype):
+    """The product that quantizes its output against the product, then the quantization."""
+    g, K, k = gen(T + F), 256, 2
+    N = 2 * F if act == "swiglu" else F
+    W = torch.stack([mx.quantize((0.1 * torch.randn((N, K), generator=g, device=DEV)).to(dtype)).codes for _ in range(E)])
+    Ws = torch.full((E, *mx.scale_shape(N, K, "block32")), 123, dtype=torch.uint8, device=DEV)
+    bias = torch.randn((E, N), generator=g, device=DEV).to(dtype)
+    X = rows_of(g, T, K, dtype)
+    r = mx.route(torch.randn((T, E), generator=g, device=DEV), k)
+    rows, space, R = mx.plan(r)
+    st, dt = torch.cuda.current_stream().cuda_stream, 0 if dtype == F16 else 1
+    q = mx._empty(R, K, "block32", DEV)
+    P = lambda t: t.data_ptr()
+    assert mx.clq_mx_quantize(P(X), dt, T, K, K, None, 1, 0, 0, P(q[0]), P(q[1]), None, P(rows), k, R, st) == 0
+    Y = torch.zeros((R, N), dtype=dtype, device=DEV)
+    assert mx.clq_mx_grouped_linear(P(q[0]), P(q[1]), None, P(space), P(W), P(Ws), None, P(bias), T, k, E, N, K, 1, 0, dt,
+                                    P(Y), st) == 0
+    a = [torch.zeros_like(t) for t in mx._empty(R, F, "block32", DEV)[:2]]
+    f = [torch.zeros_like(t) for t in a]
+    assert mx.clq_mx_quantize_rows(P(Y), dt, P(space), T, k, E, F, N, mx.ACTS[act], 0, P(a[0]), P(a[1]), None, st) == 0
+    assert mx.clq_mx_grouped_linear_act(P(q[0]), P(q[1]), P(space), P(W), P(Ws), P(bias), T, k, E, N, K, 1, dt,
+                                        mx.ACTS[act], P(f[0]), P(f[1]), st) == 0
+    used = rows.flatten().cpu().numpy()
+    va, vf = (ref.values_of(mx.MXTensor(*t))[used] for t in (a, f))
+    if act is None:
+        np.testing.assert_array_equal(va, vf)
+    # the activations differ by 2^-20 of |h| at most: a value between two codes (or a block's largest
+    # value at a power of two) within that falls either way, about one in 2^17
+    assert (va != vf).mean() < 2.0 ** -12
+    blocks = F // 32
+    pad = ref.scale_bytes(f[1], R, 4 * -(-blocks // 4))[used][:, blocks:]
+    assert np.all(pad == 0)
+
+
+def test_combine():
     g = gen(0)
     Y = torch.randn((256, 64), generator=g, device=DEV).to(F16)
     rows = torch.tensor([[3, -1], [255, 0]], dtype=torch.int32, device=DEV)

@@ -35,7 +35,7 @@ def quantize(X=P, dtype=0, M=4, K=64, ldx=64, perm=None, b=1, act=0, fmt=0, code
 
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=2), 1), (dict(fmt=2), 1), (dict(act=3), 1), (dict(act=-1), 1), (dict(M=-1), 1), (dict(rows=-1), 1),
-    (dict(X=None), 1), (dict(codes=None), 1), (dict(scales=None), 1), (dict(fmt=1), 1), (dict(out_rows=P, k=0), 1),
+    (dict(M=1 << 30, rows=1 << 30), 2), (dict(X=None), 1), (dict(codes=None), 1), (dict(scales=None), 1), (dict(fmt=1), 1), (dict(out_rows=P, k=0), 1),
     (dict(K=48), 2), (dict(K=0), 2), (dict(K=16416, ldx=16416), 2), (dict(b=3), 2), (dict(b=512), 2), (dict(b=128), 2),
     (dict(ldx=32), 2), (dict(act=2), 2), (dict(rows=3), 2),
     (dict(ldx=68), 3), (dict(X=P + 8), 3), (dict(codes=P + 8), 3), (dict(scales=P + 4), 3), (dict(perm=P + 2), 3),
@@ -46,7 +46,7 @@ def test_quantize_refuses(lib, change, code):
 
 @pytest.mark.parametrize("args,code", [
     ((P, P, None, 4, 64, 0, 2, P), 1), ((P, P, None, 4, 64, 3, 0, P), 1), ((P, P, None, -1, 64, 0, 0, P), 1),
-    ((P, P, None, 4, 40, 0, 0, P), 2), ((P, P, None, 4, 64, 1, 0, P), 1), ((P, P, None, 4, 64, 0, 0, None), 1),
+    ((P, P, None, 1 << 30, 64, 0, 0, P), 2), ((P, P, None, 4, 40, 0, 0, P), 2), ((P, P, None, 4, 64, 1, 0, P), 1), ((P, P, None, 4, 64, 0, 0, None), 1),
     ((P, P, None, 4, 64, 0, 0, P + 2), 3), ((P + 1, P, None, 4, 64, 0, 0, P), 3), ((None, None, None, 0, 64, 0, 0, None), 0)])
 def test_dequantize_refuses(lib, args, code):
     assert mx.clq_mx_dequantize(*args, None) == code
@@ -58,7 +58,7 @@ def linear(Xq=P, Xs=P, s_x=None, Wq=P, Ws=P, s_w=None, bias=None, M=4, N=8, K=64
 
 @pytest.mark.parametrize("change,code", [
     (dict(dtype=2), 1), (dict(fmt=-1), 1), (dict(M=-1), 1), (dict(N=-1), 1), (dict(Xq=None), 1), (dict(Ws=None), 1),
-    (dict(Y=None), 1), (dict(fmt=1, s_x=P), 1), (dict(fmt=1, s_w=P), 1), (dict(K=80), 2), (dict(b=128), 2), (dict(b=0), 2),
+    (dict(Y=None), 1), (dict(fmt=1, s_x=P), 1), (dict(fmt=1, s_w=P), 1), (dict(M=1 << 30), 2), (dict(N=1 << 30), 2), (dict(K=80), 2), (dict(b=128), 2), (dict(b=0), 2),
     (dict(Y=P + 8), 3), (dict(bias=P + 1), 3), (dict(Xs=P + 8), 3), (dict(Wq=P + 4), 3), (dict(fmt=1, s_x=P, s_w=P + 1), 3),
     (dict(M=0, Y=None), 0), (dict(N=0, Wq=None), 0)])
 def test_linear_refuses(lib, change, code):
@@ -98,8 +98,16 @@ def test_plan_and_grouped_refuse(lib):
                                                     E=8, N=64, K=64, b=1, fmt=0, dtype=0, Y=P) | c).values(), None)
     assert g(plan=None) == 1 and g(Y=None) == 1 and g(fmt=1) == 1 and g(dtype=4) == 1 and g(N=-1) == 1
     assert g(k=9) == 2 and g(K=50) == 2 and g(N=1 << 30) == 2 and g(plan=P + 8) == 3 and g(T=0, Xq=None) == 0
+    f = lambda **c: mx.clq_mx_grouped_linear_act(*(dict(Xq=P, Xs=P, plan=P, Wq=P, Ws=P, bias=None, T=4, k=2, E=8, N=64, K=64,
+                                                        b=1, dtype=0, act=2, Yq=P, Ys=P) | c).values(), None)
+    assert f(act=3) == 1 and f(Yq=None) == 1 and f(Ws=None) == 1 and f(N=96) == 2 and f(N=48, act=1) == 2 and f(K=40) == 2
+    assert f(N=2 * 16416) == 2 and f(Ys=P + 8) == 3 and f(T=0, Xq=None) == 0
+    q = lambda **c: mx.clq_mx_quantize_rows(*(dict(X=P, dtype=0, plan=P, T=4, k=2, E=8, K=64, ldx=128, act=2, fmt=0, codes=P,
+                                                   scales=P, row_scale=None) | c).values(), None)
+    assert q(act=-1) == 1 and q(X=None) == 1 and q(plan=None) == 1 and q(fmt=1) == 1 and q(k=9) == 2 and q(ldx=120) == 2
+    assert q(K=48) == 2 and q(ldx=132) == 3 and q(plan=P + 4) == 3 and q(T=0, X=None) == 0
     c = lambda **c: mx.clq_mx_combine(*(dict(Y=P, dtype=0, rows=P, weights=P, T=4, k=2, D=64, R=128, out=P) | c).values(), None)
-    assert c(Y=None) == 1 and c(k=0) == 1 and c(D=60) == 2 and c(out=P + 8) == 3 and c(T=0, Y=None) == 0
+    assert c(Y=None) == 1 and c(k=0) == 1 and c(D=60) == 2 and c(D=1 << 25) == 2 and c(out=P + 8) == 3 and c(T=0, Y=None) == 0
 
 
 def tensor(rows, K, fmt="block32", lead=()):
@@ -108,7 +116,17 @@ def tensor(rows, K, fmt="block32", lead=()):
                        torch.zeros(lead + (rows,)) if fmt == "block16" else None, fmt)
 
 
-def test_helpers_refuse():
+def test_helpers_refuse_host_tensors():
+    X, q = torch.zeros((4, 64), dtype=torch.float16), tensor(4, 64)
+    for call in (lambda: mx.quantize(X), lambda: mx.dequantize(q), lambda: mx.linear(q, tensor(8, 64)),
+                 lambda: mx.route(torch.zeros((4, 8)), 2), lambda: mx.MXLinear(tensor(8, 64))(X),
+                 lambda: mx.plan(mx.Routing(torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2)), 3))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
+def test_helpers_refuse(monkeypatch):
+    monkeypatch.setattr(mx, "_on_gpu", lambda *t: None)
     X = torch.zeros((4, 64), dtype=torch.float16)
     w = tensor(8, 64)
     with pytest.raises(ValueError):
@@ -174,6 +192,7 @@ CALLS = {
 @pytest.mark.parametrize("name", sorted(CALLS))
 def test_buffers_belong_to_the_calls_stream(fake, monkeypatch, name):  # noqa: F811
     log = fake.log
+    monkeypatch.setattr(mx, "_on_gpu", lambda *t: None)
     for f in mx.EXPORTS:
         if f not in ("clq_mx_plan_rows", "clq_mx_plan_bytes", "clq_mx_scale_bytes"):
             monkeypatch.setattr(mx, f, lambda *a, f=f: log.append((f, a[-1])) or 0)
