@@ -64,8 +64,9 @@ __device__ __forceinline__ float e8m0_value(uint32_t byte) {
 
 // The same to about 2^-21 of the result (of |x| for gelu), for the product's epilogue, where
 // the exact forms' 28 and 40 instructions a value took twice the tile's MMAs (65536 rows, 2048
-// channels of K = 2048: 232 us, with these 110): a code differs where a value lies that near
+// channels of K = 2048: 232 us, with these 107): a code differs where a value lies that near
 // to the middle of two.
+// (Two values an instruction where there is one.)
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -77,19 +78,37 @@ __device__ __forceinline__ float rcp_fast(float x) {
   return r;
 }
 constexpr float kLog2e = 1.44269504088896341f;
-__device__ __forceinline__ float swiglu_fast(float g, float u) {
-  return g * rcp_fast(1.f + exp2_fast(-kLog2e * g)) * u;
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 swiglu_fast(float2 g, float2 u) {
+  const float2 n = __fmul2_rn(g, both(-kLog2e));
+  const float2 d = __fadd2_rn(make_float2(exp2_fast(n.x), exp2_fast(n.y)), both(1.f));
+  return __fmul2_rn(__fmul2_rn(g, make_float2(rcp_fast(d.x), rcp_fast(d.y))), u);
 }
-// erf by the rational approximation 7.1.26 of Abramowitz and Stegun, within 1.5e-7.
-__device__ __forceinline__ float gelu_fast(float x) {
-  const float z = fabsf(x) * 0.70710678118654752f;
-  const float t = rcp_fast(fmaf(0.3275911f, z, 1.f));
-  float p = fmaf(1.061405429f, t, -1.453152027f);
-  p = fmaf(p, t, 1.421413741f);
-  p = fmaf(p, t, -0.284496736f);
-  p = fmaf(p, t, 0.254829592f) * t;
-  const float e = p * exp2_fast(-kLog2e * z * z);  // 1 - erf(z)
-  return 0.5f * (x < 0.f ? x * e : x * (2.f - e));
+// max(x, 0) - |x| / 2 (1 - erf(|x| / sqrt 2)), erf by the rational approximation 7.1.26 of
+// Abramowitz and Stegun, within 1.5e-7.
+__device__ __forceinline__ float2 gelu_fast(float2 x) {
+  const float2 a = make_float2(fabsf(x.x), fabsf(x.y));
+  const float2 z = __fmul2_rn(a, both(0.70710678118654752f));
+  const float2 d = __ffma2_rn(z, both(0.3275911f), both(1.f));
+  const float2 t = make_float2(rcp_fast(d.x), rcp_fast(d.y));
+  float2 p = __ffma2_rn(t, both(1.061405429f), both(-1.453152027f));
+  p = __ffma2_rn(p, t, both(1.421413741f));
+  p = __ffma2_rn(p, t, both(-0.284496736f));
+  p = __ffma2_rn(p, t, both(0.254829592f));
+  const float2 q = __fmul2_rn(__fmul2_rn(z, both(-kLog2e)), z);
+  const float2 e = __fmul2_rn(__fmul2_rn(p, t), make_float2(exp2_fast(q.x), exp2_fast(q.y)));
+  return __ffma2_rn(__fmul2_rn(a, both(-0.5f)), e, make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
+}
+
+// v[0 .. N) *= f.
+template <int N>
+__device__ __forceinline__ void scale_by(float* v, float f) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const float2 r = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(f, f));
+    v[i] = r.x;
+    v[i + 1] = r.y;
+  }
 }
 
 template <typename T>

@@ -12,8 +12,9 @@
 // into tensor memory by tcgen05.cp, which repeats them for the four groups of lanes.
 //
 // Roles: warp 4 copies, one lane of warp 5 issues tcgen05.cp and tcgen05.mma, warps
-// 0-3 and 6-9 take a tile out of tensor memory (32 channels and half of the columns
-// each) while the next tile's MMAs run in the other accumulator.  Every wait is bounded.
+// 0-3 and 6-9 take a tile out of tensor memory (32 channels and a share of the
+// columns each) while the next tile's MMAs run in the other accumulator.  Every wait is
+// bounded.
 #pragma once
 
 #include "gemm_common.cuh"
@@ -30,6 +31,8 @@ constexpr int TN = 128;   // output channels a CTA
 constexpr int KC = 256;   // codes of a K step: one 128-byte row
 constexpr int WARP_TMA = 4;
 constexpr int WARP_MMA = 5;
+// Eight: with sixteen the registers left to each spill (32768 x 4096 -> 8192 in blocks of 16
+// 323 -> 351 us; the experts' GELU in the epilogue 88 -> 105).
 constexpr int EPI_WARPS = 8;
 constexpr int THREADS = 32 * (EPI_WARPS + 2);
 constexpr int MAX_STAGES = 8;
@@ -54,7 +57,7 @@ struct Cfg {
   static constexpr int OFF_SA = OFF_B + S * B;
   static constexpr int OFF_SB = OFF_SA + S * SA;
   static constexpr int OFF_EPI = OFF_SB + S * SB;
-  static constexpr int BYTES = OFF_EPI + EPI_WARPS * 2 * EPI_BYTES;
+  static constexpr int BYTES = OFF_EPI + FIXED;
   // Tensor memory: two accumulators of NT columns and the scales of NSF K steps (tcgen05
   // copies and MMAs of one thread run in the order of their issue; a second buffer beside
   // 256-column accumulators would make them share more columns than two blocks: 32768 x 4096
@@ -141,6 +144,9 @@ __device__ __forceinline__ void stmatrix4_trans(uint32_t addr, const uint32_t (&
 // A tile of the output: `n0` its first channel within its matrix, `expert`'s.
 struct Tile {
   int n0, row0, rows, expert;
+  // Columns that its MMAs make: a tile that ends early takes only the time of those (the
+  // pair's CTAs hold half of them each).
+  __device__ __forceinline__ int columns(int nt) const { return min(nt, (rows + 63) / 64 * 64); }
 };
 
 __device__ __forceinline__ uint4 select(bool c, const uint4& a, const uint4& b) {
@@ -279,7 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
         const int n0 = T.n0 + rank * TN;
         const int wrow = T.expert * g.N + n0;
-        const int xrow = T.row0 + rank * (NT / CG);
+        const int xrow = T.row0 + (CG == 2 && rank != 0 ? T.columns(NT) / 2 : 0);
         const int wchunk = (T.expert * g.w_blocks + n0 / kRowBlock) * g.chunks;
         const int xchunk = T.row0 / kRowBlock * g.chunks;
         for (int kb = 0; kb < nk; ++kb, ++it) {
@@ -332,6 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const Tile T = tile_at<NT, CG, GROUPED>(g, t, tiles_n);
         // a 64-row tile may be the second half of its scale block
         const uint32_t xcol = NT == 64 ? static_cast<uint32_t>(T.row0 & 64) / 32u : 0u;
+        const uint32_t columns = static_cast<uint32_t>(T.columns(NT));
         const int buf = tc & 1;
         if (!mbar_wait_bounded(&bars.acc_empty[buf], ((tc >> 1) & 1) ^ 1, abort, g.status,
                                kWaitLimitNs) ||
@@ -367,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (k < steps) {
               const int c = FMT == CLQ_MX_BLOCK32 ? k >> 1 : k;
               const uint32_t sf = FMT == CLQ_MX_BLOCK32 ? (k & 1) * 2 : 0;
-              mma_mx<FMT, CG>(d, a0 + k * 2, b0 + k * 2, idesc_mx(FMT, TN * CG, NT, sf),
+              mma_mx<FMT, CG>(d, a0 + k * 2, b0 + k * 2, idesc_mx(FMT, TN * CG, columns, sf),
                               sfa + 4 * c, sfb + 4 * C::XB * c + xcol, (kb | k) == 0 ? 0u : 1u);
             }
           }
@@ -532,7 +539,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                             v + 8 * c);
             if (g.act == CLQ_MX_ACT_GELU) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = gelu_fast(v[i]);
+              for (int i = 0; i < 32; i += 2) {
+                const float2 y = gelu_fast(make_float2(v[i], v[i + 1]));
+                v[i] = y.x;
+                v[i + 1] = y.y;
+              }
             }
             float most = fabsf(v[0]);
 #pragma unroll
@@ -540,13 +551,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             most = absmax3(most, v[31], v[31]);
             const uint32_t byte = e8m0_byte(__float_as_uint(most));
             const float inv = e8m0_inverse(byte);
+            scale_by<32>(v, inv);
             uint32_t code[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) v[8 * c + i] = __fmul_rn(v[8 * c + i], inv);
-              code[c] = byte == 255u ? 0u : e2m1x8(v + 8 * c);
-            }
+            for (int c = 0; c < 4; ++c) code[c] = byte == 255u ? 0u : e2m1x8(v + 8 * c);
             if (lane < rows) {
               *reinterpret_cast<uint4*>(g.Yq + static_cast<size_t>(row + lane) * (g.N / 2) + n0 / 2) =
                   make_uint4(code[0], code[1], code[2], code[3]);
@@ -559,7 +567,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             pair_barrier(1 + part * 2 + (quarter >> 1));
             const int half = lane & 1, m = 16 * (quarter & 1) + (lane >> 1);
             const uint8_t* from = smem + C::OFF_EPI +
-                                  (part * 4 + (quarter & 2) + half) * 2 * EPI_BYTES + turn * EPI_BYTES;
+                                  ((part * 4 + (quarter & 2) + half) * 2 + turn) * EPI_BYTES;
             uint4 p[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c)  // the two lanes' chunks on different banks
@@ -571,7 +579,12 @@ __global__ void __launch_bounds__(THREADS, 1)
               unpack8<OutT>(select(half, p[(2 * h) ^ 2], p[2 * h]), gate);
               unpack8<OutT>(select(half, p[(2 * h + 1) ^ 2], p[2 * h + 1]), up);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) v[8 * h + i] = swiglu_fast(gate[i], up[i]);
+              for (int i = 0; i < 8; i += 2) {
+                const float2 y = swiglu_fast(make_float2(gate[i], gate[i + 1]),
+                                             make_float2(up[i], up[i + 1]));
+                v[8 * h + i] = y.x;
+                v[8 * h + i + 1] = y.y;
+              }
             }
             float most = fabsf(v[0]);
 #pragma unroll
@@ -579,8 +592,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             most = absmax3(most, v[15], __shfl_xor_sync(0xffffffffu, absmax3(most, v[15], v[15]), 1));
             const uint32_t byte = e8m0_byte(__float_as_uint(most));
             const float inv = e8m0_inverse(byte);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __fmul_rn(v[i], inv);
+            scale_by<16>(v, inv);
             uint2 code = make_uint2(e2m1x8(v), e2m1x8(v + 8));
             if (byte == 255u) code = make_uint2(0, 0);
             if (m < rows) {

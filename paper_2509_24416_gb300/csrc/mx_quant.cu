@@ -229,12 +229,7 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
       byte = bad ? 0u : e4m3_byte(__fdiv_rn(__uint_as_float(amax), __fmul_rn(6.f, srow)));
       inv = byte == 0 ? 0.f : __frcp_rn(__fmul_rn(e4m3_value(byte), srow));
     }
-#pragma unroll
-    for (int i = 0; i < U; i += 2) {
-      const float2 r = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(inv, inv));
-      v[i] = r.x;
-      v[i + 1] = r.y;
-    }
+    scale_by<U>(v, inv);
     uint2 q = make_uint2(e2m1x8(v), e2m1x8(v + 8));
     if (bad) q = make_uint2(0, 0);
     // The scale's byte, by the block's first lane; the last block's also zeroes those behind.
