@@ -406,3 +406,16 @@ def test_other_stream():
     got = layer(X, stream=s)
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+def test_example_runs(fmt):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "sparse_feed_forward.py")
+    spec = importlib.util.spec_from_file_location("sparse_feed_forward", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    # three products in a row of operands with about 10 % error each, the middle one squared by the
+    # gate: far from 1 still
+    assert m.main(["--tokens", "300", "--hidden", "512", "--ffn", "256", "--experts", "4", "--format", fmt]) < 0.7
