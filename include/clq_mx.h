@@ -39,7 +39,8 @@
  *            is 0; a row with an infinity or a NaN has s_row NaN (codes and
  *            scales 0).
  *   rn rounds to the nearest E2M1 value, ties to the even code, |.| > 6 to 6.
- * Every step is one IEEE fp32 operation in the order written.
+ * Every step is one IEEE fp32 operation in the order written; a value that is exactly 0
+ * has code 0 (not 8, its negative).
  */
 #ifndef CLQ_MX_H
 #define CLQ_MX_H

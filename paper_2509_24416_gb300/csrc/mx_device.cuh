@@ -100,12 +100,12 @@ __device__ __forceinline__ float2 gelu_fast(float2 x) {
   return __ffma2_rn(__fmul2_rn(a, both(-0.5f)), e, make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
 }
 
-// v[0 .. N) *= f.
+// v[0 .. N) *= f; plus 0, which gives a product that is exactly 0 the positive sign.
 template <int N>
 __device__ __forceinline__ void scale_by(float* v, float f) {
 #pragma unroll
   for (int i = 0; i < N; i += 2) {
-    const float2 r = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(f, f));
+    const float2 r = __ffma2_rn(make_float2(v[i], v[i + 1]), both(f), both(0.f));
     v[i] = r.x;
     v[i + 1] = r.y;
   }

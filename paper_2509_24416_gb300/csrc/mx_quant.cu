@@ -1,6 +1,5 @@
 // Rows -> E2M1 codes with block scales, and back.
-#include "mx_device.cuh"
-#include "mx_kernels.h"
+#include "mx_quant_wide.cuh"
 
 namespace clq {
 namespace mx {
@@ -346,8 +345,35 @@ cudaError_t launch_rows(void (*k)(KArgs...), int grid, int tx, int ty, size_t sm
   return cudaLaunchKernelEx(&cfg, k, args...);
 }
 
+// Many swapped rows rotated by blocks of 64 or 128 (mx_quant_wide.cuh): enough for a tile
+// and a quarter a SM, and rows long enough for bulk copies.  Measured, us, wide / 16 values a
+// thread, b = 64, BLOCK32: 1152 values a row, 512 rows 6.4 / 4.6, 1024 rows 7.0 / 7.3, 2048 rows
+// 7.9 / 9.2; 1024 rows of 2048 8.7 / 8.3, 2048 rows 10.0 / 10.8; 65536 threads' worth of rows of
+// 256 values 10.3 / 9.0, of 512 8.9 / 10.9.
+bool wide_fits(const QuantArgs& a) {
+  return a.perm != nullptr && (a.b == 64 || a.b == 128) && a.act == CLQ_MX_ACT_NONE &&
+         a.tiles == nullptr && a.K >= 512 && a.K / WIDE <= WIDE_THREADS &&
+         static_cast<int64_t>(a.M) * (a.K / WIDE) >= 5ll * WIDE_THREADS * sm_count() / 4;
+}
+
+template <typename T, int FMT>
+cudaError_t quantize_wide_t(const QuantArgs& args, cudaStream_t st) {
+  QuantArgs a = args;
+  const int per_row = a.K / WIDE;
+  a.block_rows = WIDE_THREADS / per_row;
+  const int threads = (a.block_rows * per_row + 31) / 32 * 32;
+  const size_t smem = static_cast<size_t>(WIDE_STAGES) * a.block_rows * a.K * 2;
+  auto k = a.b == 64 ? quantize_wide_kernel<T, FMT, 6> : quantize_wide_kernel<T, FMT, 7>;
+  int per_sm = 0;
+  const cudaError_t e = kernel_setup(reinterpret_cast<const void*>(k), smem, threads, &per_sm);
+  if (e != cudaSuccess) return e;
+  const int tiles = (a.M + a.block_rows - 1) / a.block_rows;
+  return launch_pdl(k, std::min(tiles, std::max(1, per_sm) * sm_count()), threads, smem, st, a);
+}
+
 template <typename T, int FMT>
 cudaError_t quantize_t(const QuantArgs& args, cudaStream_t st) {
+  if (wide_fits(args)) return quantize_wide_t<T, FMT>(args, st);
   // Rows of a block: of those with up to 512 threads the number that leaves the fewest lanes
   // idle, among equals the smallest of at least 128 threads; with few rows no more than give
   // every SM two blocks (256 x 1152: 3.1 us with one row, 3.9 with four).

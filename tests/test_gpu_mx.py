@@ -96,6 +96,40 @@ def test_quantize_rotated(fmt, M, K, b, swap):
 
 
 @pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,K,b", [(6601, 1152, 64), (6601, 1152, 128), (120003, 64, 64), (117001, 128, 128), (900, 12288, 128),
+                                   (12001, 704, 64), (2500, 4608, 64), (9001, 512, 128)])
+def test_quantize_many_rows(fmt, dtype, M, K, b):
+    """Many swapped and rotated rows take a kernel of their own: the same bytes as in small parts."""
+    g = gen(M + b)
+    big = rows_of(g, M, K + 8, dtype)
+    X = big[:, :K]
+    X[M // 3, 5], X[M // 2, 3] = float("inf"), float("nan")
+    X[M // 5] = 0
+    perm = perm_of(g, K)
+    q = mx.quantize(X, fmt, perm, b)
+    step = 128 * max(1, 60000 // K // 128)
+    parts = [mx.quantize(X[i:i + step], fmt, perm, b) for i in range(0, M, step)]
+    assert torch.equal(q.codes, torch.cat([p.codes for p in parts]))
+    blocks = 4 * -(-K // (4 * ref.BLOCK[fmt]))
+    got = ref.scale_bytes(q.scales, M, blocks)
+    np.testing.assert_array_equal(got, np.concatenate([ref.scale_bytes(p.scales, p.rows, blocks) for p in parts]))
+    if fmt == "block16":
+        want = torch.cat([p.row_scale for p in parts])
+        assert torch.equal(q.row_scale.nan_to_num(-1), want.nan_to_num(-1))
+    # into other rows, some of them twice or nowhere
+    T, k = M, 2
+    rows = torch.stack((torch.randperm(M, generator=g, device=DEV), torch.full((M,), -1, device=DEV)), 1).to(torch.int32)
+    rows[::2, 1] = M + torch.arange((M + 1) // 2, device=DEV).to(torch.int32)
+    R = M + (M + 1) // 2
+    out = mx._empty(R, K, fmt, DEV)
+    P = lambda t: None if t is None else t.data_ptr()
+    assert mx.clq_mx_quantize(P(X), 0 if dtype == F16 else 1, M, K, X.stride(0), P(perm), b, 0, mx.FORMATS[fmt], *map(P, out),
+                              P(rows), k, R, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(out[0][rows[:, 0].long()], q.codes) and torch.equal(out[0][M:], q.codes[::2])
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
 @pytest.mark.parametrize("act", ["gelu", "swiglu"])
 @pytest.mark.parametrize("M,K,b,swap", [(3, 96, 1, False), (130, 1536, 32, True)])
 def test_quantize_activation(fmt, act, M, K, b, swap):
