@@ -62,10 +62,10 @@ __device__ __forceinline__ float e8m0_value(uint32_t byte) {
   return __uint_as_float((byte << 23) | (((byte + 1u) & 0xFEu) == 0u ? 0x400000u : 0u));
 }
 
-// The same to about 2^-21 of the result (of |x| for gelu), for the product's epilogue, where
-// the exact forms' 28 and 40 instructions a value took twice the tile's MMAs (65536 rows, 2048
-// channels of K = 2048: 232 us, with these 107): a code differs where a value lies that near
-// to the middle of two.
+// Activations, within 2^-21 of |x| (of |g u| for swiglu) of the exact ones.  With erff, expf and a
+// division of full precision (28 and 40 instructions a value) quantisation was bound by
+// instructions (16384 x 4608, gelu, BLOCK16: 113 us, with these 75) and the product's epilogue
+// took twice the tile's MMAs (65536 rows, 2048 channels of K = 2048: 232 us, with these 107).
 // (Two values an instruction where there is one.)
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
@@ -84,20 +84,25 @@ __device__ __forceinline__ float2 swiglu_fast(float2 g, float2 u) {
   const float2 d = __fadd2_rn(make_float2(exp2_fast(n.x), exp2_fast(n.y)), both(1.f));
   return __fmul2_rn(__fmul2_rn(g, make_float2(rcp_fast(d.x), rcp_fast(d.y))), u);
 }
-// max(x, 0) - |x| / 2 (1 - erf(|x| / sqrt 2)), erf by the rational approximation 7.1.26 of
-// Abramowitz and Stegun, within 1.5e-7.
+// max(x, 0) - |x| / 2 erfc(|x| / sqrt 2); erfc(y) = exp(-y^2) f(t), t = 1 / (1 + 0.33 y), f t
+// times the polynomial of degree 7 with the smallest relative error up to y = 9.5 (8e-8;
+// iteratively reweighted least squares), -1 / 2 in its coefficients.  So the negative side,
+// where 1 + erf cancels, keeps its relative precision but for that of exp's argument
+// (2^-20.6 to x = -3, 2^-18 to x = -9).
 __device__ __forceinline__ float2 gelu_fast(float2 x) {
   const float2 a = make_float2(fabsf(x.x), fabsf(x.y));
-  const float2 z = __fmul2_rn(a, both(0.70710678118654752f));
-  const float2 d = __ffma2_rn(z, both(0.3275911f), both(1.f));
+  const float2 d = __ffma2_rn(a, both(0.23334524f), both(1.f));
   const float2 t = make_float2(rcp_fast(d.x), rcp_fast(d.y));
-  float2 p = __ffma2_rn(t, both(1.061405429f), both(-1.453152027f));
-  p = __ffma2_rn(p, t, both(1.421413741f));
-  p = __ffma2_rn(p, t, both(-0.284496736f));
-  p = __ffma2_rn(p, t, both(0.254829592f));
-  const float2 q = __fmul2_rn(__fmul2_rn(z, both(-kLog2e)), z);
+  float2 p = __ffma2_rn(t, both(0.0679643899f), both(-0.231344074f));
+  p = __ffma2_rn(p, t, both(0.177719399f));
+  p = __ffma2_rn(p, t, both(-0.206270739f));
+  p = __ffma2_rn(p, t, both(-0.0225053579f));
+  p = __ffma2_rn(p, t, both(-0.100961901f));
+  p = __ffma2_rn(p, t, both(-0.0914186239f));
+  p = __ffma2_rn(p, t, both(-0.0931830555f));
+  const float2 q = __fmul2_rn(__fmul2_rn(a, both(-0.5f * kLog2e)), a);
   const float2 e = __fmul2_rn(__fmul2_rn(p, t), make_float2(exp2_fast(q.x), exp2_fast(q.y)));
-  return __ffma2_rn(__fmul2_rn(a, both(-0.5f)), e, make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
+  return __ffma2_rn(a, e, make_float2(fmaxf(x.x, 0.f), fmaxf(x.y, 0.f)));
 }
 
 // v[0 .. N) *= f; plus 0, which gives a product that is exactly 0 the positive sign.
@@ -126,14 +131,6 @@ __device__ __forceinline__ float absmax3(float a, float b, float c) {
   float r;
   asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
-}
-
-// The activations, each operation rounded by itself.
-__device__ __forceinline__ float gelu(float x) {
-  return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.f, erff(__fmul_rn(x, 0.70710678118654752f))));
-}
-__device__ __forceinline__ float swiglu(float g, float u) {
-  return __fmul_rn(__fdiv_rn(g, __fadd_rn(1.f, expf(-g))), u);
 }
 
 }  // namespace mx

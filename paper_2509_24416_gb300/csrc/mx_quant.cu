@@ -154,14 +154,22 @@ __global__ void __launch_bounds__(1024) quantize_kernel(QuantArgs a) {
         unpack8<T>(raw[2 * h], g);
         unpack8<T>(raw[2 * h + 1], u);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * h + i] = swiglu(g[i], u[i]);
+        for (int i = 0; i < 8; i += 2) {
+          const float2 y = swiglu_fast(make_float2(g[i], g[i + 1]), make_float2(u[i], u[i + 1]));
+          v[8 * h + i] = y.x;
+          v[8 * h + i + 1] = y.y;
+        }
       }
     } else if constexpr (ACT == CLQ_MX_ACT_GELU || !SWAP) {
       unpack8<T>(raw[0], v);
       unpack8<T>(raw[1], v + 8);
       if (ACT == CLQ_MX_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) v[i] = gelu(v[i]);
+        for (int i = 0; i < U; i += 2) {
+          const float2 y = gelu_fast(make_float2(v[i], v[i + 1]));
+          v[i] = y.x;
+          v[i + 1] = y.y;
+        }
       }
     }
     if constexpr (SWAP) {
