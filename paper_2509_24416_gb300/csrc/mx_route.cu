@@ -15,7 +15,7 @@ constexpr int ROUTE_WARPS = 8;
 // Order-preserving bits of a float (no NaN); -0 as +0.
 __device__ __forceinline__ uint32_t ordered(float f) {
   const uint32_t u = __float_as_uint(__fadd_rn(f, 0.f));
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+  return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float unordered(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
@@ -51,23 +51,45 @@ __device__ __forceinline__ uint32_t group_sum(uint32_t a, uint32_t b, int lane, 
   return ordered(__fadd_rn(unordered(first), unordered(second)));
 }
 
+// The eighth largest of the lanes' values: eights sorted in turn down and up; the larger ones of
+// the pairs of two such neighbours are the eight largest of both.
+__device__ __forceinline__ uint32_t eighth_largest(uint32_t v, int lane) {
+  auto step = [&](int stride, int size) {
+    const uint32_t o = __shfl_xor_sync(kAll, v, stride);
+    v = ((lane & stride) == 0) == ((lane & size) == 0) ? max(v, o) : min(v, o);
+  };
+  step(1, 2);
+  step(2, 4), step(1, 4);
+  step(4, 8), step(2, 8), step(1, 8);
+  v = max(v, __shfl_xor_sync(kAll, v, 8));
+  step(4, 16), step(2, 16), step(1, 16);
+  v = max(v, __shfl_xor_sync(kAll, v, 16));
+  return __reduce_min_sync(kAll, v);
+}
+
 // The experts of the k largest keys above kMasked, in descending order, ties to the
-// lowest expert: the j-th in lane j, -1 in the other lanes.
+// lowest expert: the j-th in lane j with its p in score, -1 and 0 in the other lanes.
 //
 // The k-th largest of the 32 lanes' own largest keys is a bound that the k largest keys
 // reach, and few others do: those are brought together, one a lane, and each counts how
 // many are in front of it.  Where more than 32 reach it (many equal scores), the largest
 // is taken k times.  32768 tokens of 256 experts, k = 8: 41 us with the second way alone.
 template <int C>
-__device__ __forceinline__ int choose(uint32_t (&key)[C], int lane, int k, uint2* slots) {
+__device__ __forceinline__ int choose(uint32_t (&key)[C], const float (&p)[C], int lane, int k,
+                                      uint4* slots, float& score) {
   uint32_t top = key[0];
 #pragma unroll
   for (int i = 1; i < C; ++i) top = max(top, key[i]);
-  uint32_t bound = 0, rest = top;
-  for (int j = 0; j < k; ++j) {
-    bound = __reduce_max_sync(kAll, rest);
-    if (bound <= kMasked) break;
-    if (lane == __ffs(__ballot_sync(kAll, rest == bound)) - 1) rest = 0;
+  uint32_t bound = 0;
+  if (k > 4 && k <= 8) {
+    bound = eighth_largest(top, lane);
+  } else {
+    uint32_t rest = top;
+    for (int j = 0; j < k; ++j) {
+      bound = __reduce_max_sync(kAll, rest);
+      if (bound <= kMasked) break;
+      if (lane == __ffs(__ballot_sync(kAll, rest == bound)) - 1) rest = 0;
+    }
   }
   bound = max(bound, kMasked + 1);
   uint32_t have[C];
@@ -78,26 +100,32 @@ __device__ __forceinline__ int choose(uint32_t (&key)[C], int lane, int k, uint2
     n += __popc(have[i]);
   }
   int mine = -1;
+  score = 0.f;
   if (n <= 32) {
     // lane l takes the l-th of them in the order of the experts
     int before = 0;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
       if (key[i] >= bound)
-        slots[before + __popc(have[i] & ((1u << lane) - 1u))] = make_uint2(key[i], 32 * i + lane);
+        slots[before + __popc(have[i] & ((1u << lane) - 1u))] =
+            make_uint4(key[i], 32 * i + lane, __float_as_uint(p[i]), 0);
       before += __popc(have[i]);
     }
     __syncwarp();
-    const uint2 my = slots[lane];
+    const uint4 my = slots[lane];
     int rank = 0;
     for (int j = 0; j < n; ++j) {
       const uint32_t o = __shfl_sync(kAll, my.x, j);
       rank += o > my.x || (o == my.x && j < lane) ? 1 : 0;
     }
     __syncwarp();
-    if (lane < n && rank < k) slots[rank].y = my.y;
+    if (lane < n && rank < k) slots[rank] = my;
     __syncwarp();
-    if (lane < min(k, n)) mine = static_cast<int>(slots[lane].y);
+    if (lane < min(k, n)) {
+      const uint4 s = slots[lane];
+      mine = static_cast<int>(s.y);
+      score = __uint_as_float(s.z);
+    }
     return mine;
   }
   for (int j = 0; j < k; ++j) {
@@ -113,11 +141,57 @@ __device__ __forceinline__ int choose(uint32_t (&key)[C], int lane, int k, uint2
       if (32 * i + lane == at) key[i] = 0u;
     if (lane == j) mine = at;
   }
+  // the scores from the lanes that have them
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const float v = __shfl_sync(kAll, p[i], mine & 31);
+    if (mine >> 5 == i) score = v;
+  }
   return mine;
 }
 
+// Two largest of two pairs of them: max(a, a'), max(min(a, a'), b, b').
+__device__ __forceinline__ void two_largest(uint32_t& a, uint32_t& b, uint32_t a2, uint32_t b2) {
+  b = max(min(a, a2), max(b, b2));
+  a = max(a, a2);
+}
+
+// The same for groups of 32 regs neighbours, regs a power of two: lane g ends with group
+// g's, the others with 0.  Each of the first stages halves the registers that a lane looks
+// after, so that 9 exchanges of two words do what C = 8 groups by themselves take 16
+// reductions and 8 ballots for.
+template <int C>
+__device__ __forceinline__ uint32_t group_keys_wide(const uint32_t (&key)[C], int lane, int regs,
+                                                    int groups, bool two) {
+  uint32_t x[C], y[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) x[i] = key[i], y[i] = 0;
+  int m = 16;
+#pragma unroll
+  for (int h = C / 2; h >= 1; h /= 2, m /= 2) {
+    const bool up = lane & m;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const uint32_t x2 = __shfl_xor_sync(kAll, up ? x[i] : x[i + h], m);
+      const uint32_t y2 = h == C / 2 ? 0 : __shfl_xor_sync(kAll, up ? y[i] : y[i + h], m);
+      x[i] = up ? x[i + h] : x[i];
+      y[i] = up ? y[i + h] : y[i];
+      two_largest(x[i], y[i], x2, y2);
+    }
+  }
+#pragma unroll
+  for (; m >= 1; m /= 2)
+    two_largest(x[0], y[0], __shfl_xor_sync(kAll, x[0], m), __shfl_xor_sync(kAll, y[0], m));
+  constexpr int LANES = 32 / C;  // that hold one register's
+  for (m = LANES; m < LANES * regs; m *= 2)
+    two_largest(x[0], y[0], __shfl_xor_sync(kAll, x[0], m), __shfl_xor_sync(kAll, y[0], m));
+  const uint32_t g = two ? ordered(__fadd_rn(unordered(x[0]), unordered(y[0]))) : x[0];
+  const uint32_t mine = __shfl_sync(kAll, g, lane * LANES * regs);
+  return lane < groups ? mine : 0u;
+}
+
 // The same for groups of 32 / 2^n neighbours: each lane ends with its group's, in
-// every register.  Two largest of a pair of pairs: max(a, a'), max(min(a, a'), b, b').
+// every register.
 template <int C>
 __device__ __forceinline__ void group_keys_narrow(const uint32_t (&key)[C], int size, bool two,
                                                   uint32_t (&g)[C]) {
@@ -126,16 +200,17 @@ __device__ __forceinline__ void group_keys_narrow(const uint32_t (&key)[C], int 
     uint32_t a = key[i], b = 0;
     for (int m = 1; m < size; m *= 2) {
       const uint32_t a2 = __shfl_xor_sync(kAll, a, m), b2 = __shfl_xor_sync(kAll, b, m);
-      b = max(min(a, a2), max(b, b2));
-      a = max(a, a2);
+      two_largest(a, b, a2, b2);
     }
     g[i] = two ? ordered(__fadd_rn(unordered(a), unordered(b))) : a;
   }
 }
 
-// One warp a token, 32 C >= E; keys in registers.  Bound by integer instructions.
+// One warp a token, 32 C >= E; keys in registers.  Bound by instructions (some 800 a token) and
+// the chains of exchanges, which five blocks a SM cover best (four, six: 4 % slower).  32768
+// tokens of 256 experts, k = 8, sigmoid, 4 of 8 groups kept: 30.1 us; without groups 23.8.
 template <typename T, int C>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, C <= 8 ? 5 : 1) route_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
   pdl_wait();
@@ -149,7 +224,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
   for (int i = 0; i < C; ++i) {
     const int e = 32 * i + lane;
     const float x = e < a.E ? load_logit<T>(a.logits, static_cast<size_t>(t) * a.ld + e) : -INFINITY;
-    masked[i] = x == -INFINITY || x != x;
+    masked[i] = !(x > -INFINITY);  // a NaN too
     p[i] = fminf(x, FLT_MAX);
     if (!masked[i]) most = fmaxf(most, p[i]);
   }
@@ -173,7 +248,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
     for (int i = 0; i < C; ++i) p[i] = __fdiv_rn(p[i], s[0]);
   } else {
 #pragma unroll
-    for (int i = 0; i < C; ++i) p[i] = __fdiv_rn(1.f, __fadd_rn(1.f, expf(-p[i])));
+    for (int i = 0; i < C; ++i) p[i] = __frcp_rn(__fadd_rn(1.f, expf(-p[i])));
   }
 #pragma unroll
   for (int i = 0; i < C; ++i) {
@@ -186,7 +261,9 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
     const int size = a.E / a.groups;
     const bool two = a.group_top == 2 && size > 1;
     uint32_t gkey = 0;  // lane g: group g (at most 32)
-    if (size % 32 == 0) {
+    if (size % 32 == 0 && (size & (size - 1)) == 0) {
+      gkey = group_keys_wide<C>(key, lane, size / 32, a.groups, two);
+    } else if (size % 32 == 0) {
       const int regs = size / 32;  // registers of a group
       uint32_t x = 0, y = 0;       // this lane's two largest of the group
       int g = 0, left = regs;
@@ -241,15 +318,9 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_kernel(RouteArgs a) {
       if (!((keep >> ((e * inv) >> 20)) & 1u)) key[i] = kMasked;
     }
   }
-  __shared__ uint2 slots[ROUTE_WARPS][32];
-  const int mine = choose<C>(key, lane, a.k, slots[threadIdx.x >> 5]);
-  // the chosen expert's score, from the lane that has it
-  float w = 0.f;
-#pragma unroll
-  for (int i = 0; i < C; ++i) {
-    const float v = __shfl_sync(kAll, p[i], mine & 31);
-    if (mine >> 5 == i) w = v;
-  }
+  __shared__ uint4 slots[ROUTE_WARPS][32];
+  float w;
+  const int mine = choose<C>(key, p, lane, a.k, slots[threadIdx.x >> 5], w);
   float total = w;
 #pragma unroll
   for (int o = 16; o >= 1; o /= 2) total = __fadd_rn(total, __shfl_xor_sync(kAll, total, o));
