@@ -48,7 +48,7 @@ struct RowTile {
 // 128 / 256 rows of one expert, counts[0] / counts[1] of them.
 struct PlanLayout {
   size_t counts_off, tiles128_off, tiles256_off, start_off, hist_off, prefix_off, bytes;
-  int max128, max256, chunks;
+  int max128, max256, chunks, pitch;
 };
 PlanLayout plan_layout(int T, int k, int E);
 inline int plan_rows(int T, int k, int E) {

@@ -210,7 +210,7 @@ __device__ __forceinline__ void group_keys_narrow(const uint32_t (&key)[C], int 
 // the chains of exchanges, which five blocks a SM cover best (four, six: 4 % slower).  32768
 // tokens of 256 experts, k = 8, sigmoid, 4 of 8 groups kept: 30.1 us; without groups 23.8.
 template <typename T, int C>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS, C <= 8 ? 5 : 1) route_kernel(RouteArgs a) {
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, C <= 8 ? 5 : 3) route_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
   pdl_wait();
@@ -333,6 +333,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, C <= 8 ? 5 : 1) route_kernel
 
 // ------------------------------------------------------------------- plan ---
 constexpr int CHUNK = 32;  // tokens a bit mask holds
+constexpr int WORDS = 4;   // masks a block of the histogram and of the rows looks after
 constexpr int PLAN_THREADS = 512;
 
 // Rows of experts e = threadIdx.x .. < E with counts[e] rows each: where each starts,
@@ -373,44 +374,69 @@ __device__ void plan_tiles(int count, int E, int32_t* start, int32_t* counts, Ro
   }
 }
 
-// Chunk c: hist[e][c] = tokens of the chunk that name expert e.
-__global__ void __launch_bounds__(256) plan_hist_kernel(const int32_t* __restrict__ experts, int T,
-                                                        int k, int E, int chunks,
-                                                        uint8_t* __restrict__ hist) {
-  extern __shared__ uint32_t mask[];  // [E]
-  pdl_wait();
-  pdl_launch_dependents();
-  for (int e = threadIdx.x; e < E; e += blockDim.x) mask[e] = 0;
+// mask[w][e]: which of the CHUNK tokens from t0 + w CHUNK name expert e.
+__device__ void expert_masks(const int32_t* __restrict__ experts, int t0, int T, int k, int E,
+                             uint32_t* mask) {
+  for (int i = threadIdx.x; i < WORDS * E; i += blockDim.x) mask[i] = 0;
   __syncthreads();
-  const int t0 = blockIdx.x * CHUNK;
-  const int n = min(CHUNK, T - t0) * k;
+  const int n = min(WORDS * CHUNK, T - t0) * k;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int e = __ldg(experts + static_cast<size_t>(t0) * k + i);
-    if (e >= 0 && e < E) atomicOr(&mask[e], 1u << (i / k));
+    const int e = __ldg(experts + static_cast<size_t>(t0) * k + i), t = i / k;
+    if (e >= 0 && e < E) atomicOr(&mask[t / CHUNK * E + e], 1u << (t % CHUNK));
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += blockDim.x)
-    hist[static_cast<size_t>(e) * chunks + blockIdx.x] = static_cast<uint8_t>(__popc(mask[e]));
 }
 
-// One warp an expert: prefix[e][c] = rows of e in the chunks before c, count[e].
-__global__ void plan_prefix_kernel(const uint8_t* __restrict__ hist, int E, int chunks,
-                                   int32_t* __restrict__ prefix, int32_t* __restrict__ count) {
+// Block c: hist[e][c] = tokens of its WORDS CHUNK that name expert e; rows of `pitch` bytes,
+// zeros behind the last block's.
+__global__ void __launch_bounds__(PLAN_THREADS)
+    plan_hist_kernel(const int32_t* __restrict__ experts, int T, int k, int E, int pitch,
+                     uint8_t* __restrict__ hist) {
+  extern __shared__ uint32_t mask[];  // [WORDS][E]
+  pdl_wait();
+  pdl_launch_dependents();
+  const int c = blockIdx.x;
+  expert_masks(experts, c * WORDS * CHUNK, T, k, E, mask);
+  for (int e = threadIdx.x; e < E; e += blockDim.x) {
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) n += __popc(mask[w * E + e]);
+    uint8_t* h = hist + static_cast<size_t>(e) * pitch;
+    h[c] = static_cast<uint8_t>(n);
+    if (c == static_cast<int>(gridDim.x) - 1)
+      for (int i = c + 1; i < pitch; ++i) h[i] = 0;
+  }
+}
+
+// One warp an expert, four blocks' counts a lane: prefix[e][c] = rows of e in the blocks before
+// c, count[e].  (With one count a lane and 32 tokens a block, 32768 tokens of 256 experts, k = 8,
+// took 20.6 us for 16.7; with this inside plan_start_kernel's one block 24.6, and 9.2 for 8.7 at
+// 8192 tokens of 64.)
+__global__ void __launch_bounds__(256)
+    plan_prefix_kernel(const uint8_t* __restrict__ hist, int E, int pitch,
+                       int32_t* __restrict__ prefix, int32_t* __restrict__ count) {
   const int e = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   pdl_wait();
   pdl_launch_dependents();
   if (e >= E) return;
+  const uint32_t* h = reinterpret_cast<const uint32_t*>(hist + static_cast<size_t>(e) * pitch);
+  int4* out = reinterpret_cast<int4*>(prefix + static_cast<size_t>(e) * pitch);
+  const int words = pitch / 4;
   int carry = 0;
-  for (int c0 = 0; c0 < chunks; c0 += 32) {
-    const int c = c0 + lane;
-    const int n = c < chunks ? hist[static_cast<size_t>(e) * chunks + c] : 0;
-    int s = n;
+  uint32_t next = lane < words ? h[lane] : 0;
+  for (int c = lane; c - lane < words; c += 32) {
+    const uint32_t n = next;
+    next = c + 32 < words ? h[c + 32] : 0;
+    const int n0 = n & 0xFF, n1 = n >> 8 & 0xFF, n2 = n >> 16 & 0xFF, n3 = n >> 24;
+    int s = n0 + n1 + n2 + n3;
+    const int own = s;
     for (int o = 1; o < 32; o *= 2) {
       const int x = __shfl_up_sync(kAll, s, o);
       if (lane >= o) s += x;
     }
-    if (c < chunks) prefix[static_cast<size_t>(e) * chunks + c] = carry + s - n;
+    const int before = carry + s - own;
+    if (c < words) out[c] = make_int4(before, before + n0, before + n0 + n1, before + n0 + n1 + n2);
     carry += __shfl_sync(kAll, s, 31);
   }
   if (lane == 0) count[e] = carry;
@@ -425,29 +451,28 @@ __global__ void __launch_bounds__(PLAN_THREADS)
   plan_tiles(n, E, start, counts, t128, t256);
 }
 
-__global__ void __launch_bounds__(256)
-    plan_rows_kernel(const int32_t* __restrict__ experts, int T, int k, int E, int chunks,
+__global__ void __launch_bounds__(PLAN_THREADS)
+    plan_rows_kernel(const int32_t* __restrict__ experts, int T, int k, int E, int pitch,
                      const int32_t* __restrict__ prefix, const int32_t* __restrict__ start,
                      int32_t* __restrict__ rows) {
-  extern __shared__ uint32_t mask[];  // [E]
+  extern __shared__ uint32_t mask[];  // [WORDS][E]
   pdl_wait();
   pdl_launch_dependents();
-  for (int e = threadIdx.x; e < E; e += blockDim.x) mask[e] = 0;
-  __syncthreads();
-  const int t0 = blockIdx.x * CHUNK;
-  const int n = min(CHUNK, T - t0) * k;
+  const int c = blockIdx.x, t0 = c * WORDS * CHUNK;
+  expert_masks(experts, t0, T, k, E, mask);
+  const int n = min(WORDS * CHUNK, T - t0) * k;
   const size_t at = static_cast<size_t>(t0) * k;
   for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int e = __ldg(experts + at + i);
-    if (e >= 0 && e < E) atomicOr(&mask[e], 1u << (i / k));
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const int e = __ldg(experts + at + i);
+    const int e = __ldg(experts + at + i), t = i / k;
     int r = -1;
-    if (e >= 0 && e < E)
-      r = start[e] + prefix[static_cast<size_t>(e) * chunks + blockIdx.x] +
-          __popc(mask[e] & ((1u << (i / k)) - 1u));
+    if (e >= 0 && e < E) {
+      r = start[e] + prefix[static_cast<size_t>(e) * pitch + c];
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) {  // the tokens before t
+        const int bits = min(max(t - w * CHUNK, 0), 32);
+        r += __popc(mask[w * E + e] & static_cast<uint32_t>((1ull << bits) - 1ull));
+      }
+    }
     rows[at + i] = r;
   }
 }
@@ -548,7 +573,9 @@ PlanLayout plan_layout(int T, int k, int E) {
   PlanLayout p{};
   const int64_t n = static_cast<int64_t>(T) * k;
   const int64_t used = std::min<int64_t>(E, n);
-  p.chunks = (T + CHUNK - 1) / CHUNK;
+  const int masks = (T + CHUNK - 1) / CHUNK;
+  p.chunks = masks <= SMALL_CHUNKS ? masks : (masks + WORDS - 1) / WORDS;
+  p.pitch = (p.chunks + 3) / 4 * 4;
   p.max128 = plan_rows(T, k, E) / kRowBlock;
   p.max256 = static_cast<int>((n + 255 * used) / 256);
   size_t off = 0;
@@ -561,9 +588,9 @@ PlanLayout plan_layout(int T, int k, int E) {
   p.tiles128_off = take(static_cast<size_t>(p.max128) * sizeof(RowTile));
   p.tiles256_off = take(static_cast<size_t>(p.max256) * sizeof(RowTile));
   p.start_off = take(static_cast<size_t>(2 * E) * 4);  // starts, then row counts
-  if (p.chunks > SMALL_CHUNKS) {
-    p.hist_off = take(static_cast<size_t>(E) * p.chunks);
-    p.prefix_off = take(static_cast<size_t>(E) * p.chunks * 4);
+  if (masks > SMALL_CHUNKS) {
+    p.hist_off = take(static_cast<size_t>(E) * p.pitch);
+    p.prefix_off = take(static_cast<size_t>(E) * p.pitch * 4);
   }
   p.bytes = off;
   return p;
@@ -582,23 +609,23 @@ cudaError_t launch_plan(const int32_t* experts, int T, int k, int E, int32_t* ou
   int32_t* start = reinterpret_cast<int32_t*>(p + pl.start_off);
   RowTile* t128 = reinterpret_cast<RowTile*>(p + pl.tiles128_off);
   RowTile* t256 = reinterpret_cast<RowTile*>(p + pl.tiles256_off);
-  if (pl.chunks <= SMALL_CHUNKS)  // at most 16 * 512 masks of 4 bytes: 32 KB
+  if (pl.hist_off == 0)  // at most 16 * 512 masks of 4 bytes: 32 KB
     return launch_pdl(plan_small_kernel, 1, PLAN_THREADS,
                       static_cast<size_t>(pl.chunks) * E * 4, st, experts, T, k, E, pl.chunks,
                       start, counts, t128, t256, out_rows);
   uint8_t* hist = p + pl.hist_off;
   int32_t* prefix = reinterpret_cast<int32_t*>(p + pl.prefix_off);
-  const size_t smem = static_cast<size_t>(E) * 4;
-  cudaError_t e = launch_pdl(plan_hist_kernel, pl.chunks, 256, smem, st, experts, T, k, E,
-                             pl.chunks, hist);
+  const size_t smem = static_cast<size_t>(WORDS) * E * 4;
+  cudaError_t e = launch_pdl(plan_hist_kernel, pl.chunks, PLAN_THREADS, smem, st, experts, T, k,
+                             E, pl.pitch, hist);
   if (e != cudaSuccess) return e;
   e = launch_pdl(plan_prefix_kernel, (E + 7) / 8, 256, 0, st, const_cast<const uint8_t*>(hist), E,
-                 pl.chunks, prefix, start + E);
+                 pl.pitch, prefix, start + E);
   if (e != cudaSuccess) return e;
   e = launch_pdl(plan_start_kernel, 1, PLAN_THREADS, 0, st, const_cast<const int32_t*>(start + E),
                  E, start, counts, t128, t256);
   if (e != cudaSuccess) return e;
-  return launch_pdl(plan_rows_kernel, pl.chunks, 256, smem, st, experts, T, k, E, pl.chunks,
+  return launch_pdl(plan_rows_kernel, pl.chunks, PLAN_THREADS, smem, st, experts, T, k, E, pl.pitch,
                     const_cast<const int32_t*>(prefix), const_cast<const int32_t*>(start),
                     out_rows);
 }
