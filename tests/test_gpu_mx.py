@@ -142,6 +142,43 @@ def test_quantize_activation(fmt, act, M, K, b, swap):
     check_quantized(mx.quantize(X, fmt, perm, b, act), v, slack=2.0 ** -18)
 
 
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+def test_quantize_gelu_tail(fmt):
+    """Blocks of nothing but GELU's negative side, where 1 + erf would cancel."""
+    K = 512
+    X = -3 - 6 * torch.rand((40, K), generator=gen(2), device=DEV)
+    X[:20] = X[:20].sort(1).values  # blocks of like sizes
+    X = X.to(BF16)
+    # exp's argument, up to 40, is rounded three times: 3 * 40 * 2^-24 of the value, and 2^-21 of it
+    # for the rest
+    check_quantized(mx.quantize(X, fmt, act="gelu"), ref.act(to64(X), "gelu"), slack=2.0 ** -17)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+def test_quantize_activation_extremes(fmt, act):
+    K = 96
+    low, big = torch.finfo(BF16).min, torch.finfo(BF16).max
+    X = torch.ones((5, 2 * K if act == "swiglu" else K), dtype=BF16, device=DEV)
+    X[0, 1] = low  # nothing is left of it; its neighbours are as they would be
+    X[1, 1] = big
+    X[2, 1] = float("inf")
+    X[3, 1] = float("nan")
+    q = mx.quantize(X, fmt, act=act)
+    v = mx.dequantize(q)
+    one = ref.act(to64(X[4:]), act)[0, 0]
+    assert v[0, 1] == 0 and q.codes[0, 0] >> 4 in (0, 8)
+    unit = 2.0 ** -3 if fmt == "block32" else 2.0 ** -4  # of the largest, half a step between 4 and 6
+    assert torch.all((v[0, 2:].double() - one).abs() <= unit * one) and torch.all((v[4].double() - one).abs() <= unit * one)
+    if fmt == "block32":  # 1.99 * 2^127 is nearest to 4 * 2^126, which a float does not hold
+        assert ref.scale_bytes(q.scales, 5, 3)[1, 0] == 253 and q.codes[1, 0] >> 4 == 6
+    else:
+        assert torch.isfinite(v[1]).all() and v[1, 1] >= 0.8 * big
+    for row in (2, 3):
+        first = 32 if fmt == "block32" else K
+        assert v[row, :first].isnan().all() and torch.isfinite(v[row, first:]).all()
+
+
 def test_quantize_extremes():
     K = 96
     X = torch.zeros((6, K), dtype=BF16, device=DEV)
