@@ -7,9 +7,11 @@
 // Every value passes through the operations of the loop with 16 values a thread
 // (mx_quant.cu) and has its bits.  Bound by the reads of the swap (a random one meets some
 // 3.5 to a bank) and the latencies that twelve warps a SM leave.  Measured, us, BLOCK32, a
-// random swap, here / with 16 values a thread: 8192 x 1152, b = 64, 12.8 / 16.9, b = 128
+// random swap, here / with 16 values a thread: 8192 x 1152, b = 64, 12.3 / 16.9, b = 128
 // 12.9 / 18.0; 16384 x 4608 61 / 91 (3.1 TB/s) and 64 / 99, with neighbours left together
-// 61 / 76.
+// 59 / 76.  Into eight rows each (8192 x 2048) 33.5 / 37.4: there the scales' stores count, so
+// a thread's leave together (b = 128: a pair's; a byte each took 44.5), its codes in one
+// store of 32 bytes (two of 16: 38.2).
 #pragma once
 
 #include "mx_device.cuh"
@@ -189,7 +191,6 @@ __global__ void __launch_bounds__(WIDE_THREADS, 2) quantize_wide_kernel(QuantArg
       // used again in two tiles' time, behind the next tile's barrier
       if (on && x == 0) row_max[slot == 2 ? 0 : slot + 1][y] = 0;
     }
-    if (!live) continue;
     float srow = 0.f;
     const bool bad_row = rmax >= 0x7F800000u;
     if (FMT == CLQ_MX_BLOCK16)
@@ -225,10 +226,18 @@ __global__ void __launch_bounds__(WIDE_THREADS, 2) quantize_wide_kernel(QuantArg
         w[q * C + c] = bad ? 0u : e2m1x8(f);
       }
     }
+    if (LOGB == 7) {  // whole chunks of four scales: BLOCK32 the even lane's, BLOCK16 one each
+      const uint32_t o = __shfl_xor_sync(0xffffffffu, word, 1);
+      word = FMT == CLQ_MX_BLOCK32 ? __byte_perm(word, o, 0x5140)
+             : (lane & 1)          ? __byte_perm(word, o, 0x3276)
+                                   : __byte_perm(word, o, 0x5410);
+    }
+    if (!live) continue;
     // Registers 0 .. 15 hold 32 positions from `first`, the others those `apart` behind.
     const int first = LOGB == 6 ? x * WIDE : (x >> 1) * 128 + (x & 1) * 32;
     constexpr int apart = LOGB == 6 ? 32 : 64;
     const int n = a.out_rows == nullptr ? 1 : a.k;
+    const bool whole = (reinterpret_cast<uintptr_t>(a.codes) & 31) == 0;  // one 32-byte store
     for (int j = 0; j < n; ++j) {
       const int to = a.out_rows == nullptr ? row : __ldg(a.out_rows + static_cast<size_t>(row) * a.k + j);
       if (to < 0) continue;
@@ -237,25 +246,27 @@ __global__ void __launch_bounds__(WIDE_THREADS, 2) quantize_wide_kernel(QuantArg
         continue;
       }
       uint8_t* q = a.codes + static_cast<size_t>(to) * (a.K / 2) + first / 2;
-      *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-      *reinterpret_cast<uint4*>(q + apart / 2) = make_uint4(w[4], w[5], w[6], w[7]);
+      if (LOGB == 6 && whole) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q), "r"(w[0]),
+                     "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+      } else {
+        *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(q + apart / 2) = make_uint4(w[4], w[5], w[6], w[7]);
+      }
       uint8_t* p = a.scales + static_cast<size_t>(to / kRowBlock) * chunks * 512 + (to & 31) * 16 +
                    ((to >> 5) & 3) * 4;
-      if (FMT == CLQ_MX_BLOCK16) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {  // two blocks each
-          const int blk = (first + h * apart) / 16;
-          *reinterpret_cast<uint16_t*>(p + (blk >> 2) * 512 + (blk & 3)) =
-              static_cast<uint16_t>(word >> (16 * h));
+      if (LOGB == 6) {  // all of them neighbours
+        if (FMT == CLQ_MX_BLOCK16) {
+          *reinterpret_cast<uint32_t*>(p + x * 512) = word;
+        } else {
+          *reinterpret_cast<uint16_t*>(p + (x >> 1) * 512 + 2 * (x & 1)) = static_cast<uint16_t>(word);
+          if (x == per_row - 1 && (x & 1) == 0)  // behind the last block: zeros
+            *reinterpret_cast<uint16_t*>(p + (x >> 1) * 512 + 2) = 0;
         }
-      } else {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int blk = (first + h * apart) / 32;
-          p[(blk >> 2) * 512 + (blk & 3)] = static_cast<uint8_t>(word >> (8 * h));
-        }
-        if (LOGB == 6 && x == per_row - 1 && (x & 1) == 0)  // behind the last block: zeros
-          *reinterpret_cast<uint16_t*>(p + (2 * x >> 2) * 512 + 2) = 0;
+      } else if ((x & 1) == 0 || FMT == CLQ_MX_BLOCK16) {
+        const int chunk = FMT == CLQ_MX_BLOCK16 ? x : x >> 1;
+        *reinterpret_cast<uint32_t*>(p + chunk * 512) = word;
       }
       if (FMT == CLQ_MX_BLOCK16 && x == 0) a.row_scale[to] = srow;
     }
