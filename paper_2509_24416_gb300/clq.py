@@ -325,11 +325,13 @@ def _with_stream(stream, fn, *args):
     """fn(*args) with `stream` current, so that the buffers it allocates come from that
     stream's pool: a block of the caller's stream could still be in use there, or be
     handed out again, while kernels on `stream` work on it.  New results are recorded
-    on the caller's stream, which may read and drop them."""
+    on the caller's stream, which may read and drop them: tensors, tuples of them, or
+    objects that name theirs (`_tensors`)."""
     here = torch.cuda.current_stream()
     with torch.cuda.stream(_torch_stream(stream)):
         out = fn(*args)
-    _record([t for t in (out if isinstance(out, tuple) else (out,))
+    made = out._tensors() if hasattr(out, "_tensors") else out
+    _record([t for t in (made if isinstance(made, tuple) else (made,))
              if not any(t is a for a in args)], here)
     return out
 

@@ -168,6 +168,9 @@ class MXTensor:
         t.rows, t.K = codes.shape[0], 2 * codes.shape[1]
         return t
 
+    def _tensors(self):
+        return self.codes, self.scales, self.row_scale
+
 
 def _empty(rows, K, fmt, device):
     return (torch.empty((rows, K // 2), dtype=torch.uint8, device=device),
@@ -309,6 +312,9 @@ class Routing:
         r = cls.__new__(cls)
         r.experts, r.weights, r.E = experts, weights, E
         return r
+
+    def _tensors(self):
+        return self.experts, self.weights
 
 
 def route(logits, k, scoring="softmax", balance=None, groups=1, top_groups=1, group_top=2,

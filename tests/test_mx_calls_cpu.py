@@ -1,0 +1,46 @@
+"""CPU-only checks of the microscaled calls: what a call with an explicit stream hands back to the
+caller's stream, and what calls refuse."""
+import pytest
+import torch
+
+from paper_2509_24416_gb300 import clq, mx
+from test_streams_cpu import HERE, FakeStream, fake  # noqa: F401
+from test_mx_cpu import tensor
+
+
+@pytest.fixture
+def recorded(fake, monkeypatch):  # noqa: F811
+    """Calls of the library are fakes; the (data_ptr, stream) pairs that a call records."""
+    monkeypatch.setattr(mx, "_on_gpu", lambda *t: None)
+    for f in mx.EXPORTS:
+        monkeypatch.setattr(mx, f, lambda *a: 0)
+    monkeypatch.setattr(mx, "clq_mx_plan_rows", lambda *a: 128)
+    monkeypatch.setattr(mx, "clq_mx_plan_bytes", lambda *a: 256)
+    seen = []
+    monkeypatch.setattr(clq, "_record", lambda ts, s: seen.extend(
+        (t.data_ptr(), s.cuda_stream) for t in ts if isinstance(t, torch.Tensor)))
+    return seen
+
+
+X = torch.zeros((4, 64), dtype=torch.bfloat16)
+ROUTING = mx.Routing(torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2)), 3)
+RESULTS = {
+    "quantize_block32": (lambda s: mx.quantize(X, "block32", stream=s), lambda q: [q.codes, q.scales]),
+    "quantize_block16": (lambda s: mx.quantize(X, "block16", stream=s), lambda q: [q.codes, q.scales, q.row_scale]),
+    "route": (lambda s: mx.route(torch.zeros((4, 8)), 2, stream=s), lambda r: [r.experts, r.weights]),
+    "plan": (lambda s: mx.plan(ROUTING, stream=s), lambda r: [r[0], r[1]]),
+    "dequantize": (lambda s: mx.dequantize(tensor(4, 64), stream=s), lambda y: [y]),
+    "linear": (lambda s: mx.linear(tensor(4, 64), tensor(8, 64), stream=s), lambda y: [y]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(RESULTS))
+def test_results_are_recorded_on_the_callers_stream(fake, recorded, name):  # noqa: F811
+    """The caller may read and drop what a call on another stream made: every tensor of it."""
+    call, parts = RESULTS[name]
+    out = call(fake.side)
+    assert sorted(recorded) == sorted((t.data_ptr(), HERE) for t in parts(out))
+    recorded.clear()
+    call(None)
+    call(FakeStream(HERE, fake.log))
+    assert not recorded
