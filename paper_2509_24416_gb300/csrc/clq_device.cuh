@@ -40,14 +40,22 @@ __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
 // Programmatic dependent launch.  A kernel launched with programmatic stream
 // serialization may start while the previous kernel on the stream is still
 // finishing; pdl_wait() blocks until that kernel has completed and its writes
-// are visible, so nothing global may be read before it.  Without such a
-// launch it returns at once.  pdl_launch_dependents() lets the next kernel
+// are visible, so nothing global may be read before it (but for hints, by
+// ld_relaxed).  Without such a launch it returns at once.  pdl_launch_dependents() lets the next kernel
 // (if launched that way) start as this grid's CTAs retire.
 __device__ __forceinline__ void pdl_wait() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 __device__ __forceinline__ void pdl_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// A word that another kernel may be writing: some value of it, from L2, and no line of
+// it in L1.
+__device__ __forceinline__ int32_t ld_relaxed(const int32_t* p) {
+  int32_t v;
+  asm volatile("ld.relaxed.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
 }
 
 __device__ __forceinline__ void fence_mbarrier_init() {

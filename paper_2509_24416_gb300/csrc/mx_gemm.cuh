@@ -169,13 +169,24 @@ __device__ __forceinline__ void store_scale(const GemmArgs& g, int row, int blk,
     for (int q = (blk & 3) + 1; q < 4; ++q) s[q] = 0;
 }
 
+// One tile of the list into L1.
+__device__ __forceinline__ void fetch_line(const RowTile* p) {
+  int4 e;
+  asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(e.x), "=r"(e.y), "=r"(e.z), "=r"(e.w)
+               : "l"(p)
+               : "memory");
+}
+
 template <int NT, int CG, bool GROUPED>
 __device__ __forceinline__ Tile tile_at(const GemmArgs& g, int t, int tiles_n) {
   const int m = t / tiles_n;
   Tile r;
   r.n0 = (t - m * tiles_n) * (TN * CG);
   if (GROUPED) {
-    const int4 e = __ldg(reinterpret_cast<const int4*>(g.tiles) + m);
+    // (an ordinary load: the plan may be written while this CTA waits for it, which a
+    // read-only one must not be used for)
+    const int4 e = reinterpret_cast<const int4*>(g.tiles)[m];
     r.expert = e.x;
     r.row0 = e.y;
     r.rows = e.z;
@@ -251,13 +262,14 @@ __global__ void __launch_bounds__(THREADS, 1)
   // While the previous kernel finishes, this CTA's first weights are on their way into L2:
   // few rows meet many experts' weights, whose bytes are the work (8 tokens through 6 of 64
   // experts: 30.1 us, with these 27.3; a dense layer's weights are often in L2 already, and
-  // the hints cost 1 x 4096 -> 16384 a microsecond).  Whatever the plan's list holds at
-  // this time, a hint changes no value.
+  // the hints cost 1 x 4096 -> 16384 a microsecond).  The plan's list may still be in the
+  // writing: whatever it holds by now, a hint changes no value, and the relaxed load leaves no
+  // old line behind for the loads after the wait.
   if (GROUPED && NT <= 128 && warp == WARP_TMA) {
     if (elect_one()) {
       const int t = static_cast<int>(blockIdx.x);
-      const int expert =
-          min(max(g.tiles[min(t / tiles_n, g.max_tiles - 1)].expert, 0), g.experts - 1);
+      const int expert = min(max(ld_relaxed(&g.tiles[min(t / tiles_n, g.max_tiles - 1)].expert), 0),
+                             g.experts - 1);
       const int n0 = t % tiles_n * TN;
       for (int kb = 0; kb < nk; ++kb) {
         tma_prefetch_2d(&mapW, kb * 128, expert * g.N + n0);
@@ -270,8 +282,10 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_launch_dependents();
 
   volatile int32_t* abort = &bars.abort;
-  const int tiles = (GROUPED ? __ldg(g.tile_count) : (g.M + NT - 1) / NT) * tiles_n;
   const int unit = static_cast<int>(blockIdx.x) / CG;
+  // this CTA's first tile on its way beside the list's length (the list has room for it)
+  if (GROUPED) fetch_line(g.tiles + unit / tiles_n);
+  const int tiles = (GROUPED ? *g.tile_count : (g.M + NT - 1) / NT) * tiles_n;
   const int units = static_cast<int>(gridDim.x) / CG;
   const int rank = CG == 2 ? static_cast<int>(cluster_ctarank()) : 0;
 
