@@ -133,5 +133,24 @@ __device__ __forceinline__ float absmax3(float a, float b, float c) {
   return r;
 }
 
+// Barrier of two warps (of its number's 64 threads).
+__device__ __forceinline__ void pair_barrier(int id) {
+  asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+}
+
+// The same, and whether all of them had `ok`.
+__device__ __forceinline__ bool pair_all(int id, bool ok) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %2, 0;\n\t"
+      "barrier.cta.red.and.pred q, %1, 64, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(id), "r"(static_cast<uint32_t>(ok))
+      : "memory");
+  return r != 0;
+}
+
 }  // namespace mx
 }  // namespace clq
