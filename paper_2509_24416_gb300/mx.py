@@ -142,7 +142,8 @@ def _on_gpu(*tensors):
 class MXTensor:
     """Rows of E2M1 codes: ``codes`` uint8 [.., rows, K / 2], ``scales`` uint8 [.., *scale_shape]
     and, for "block16", ``row_scale`` fp32 [.., rows]; a leading dimension is a stack (of experts'
-    weights).  Code bytes that come in a wider integer type are narrowed here, once."""
+    weights).  Code bytes that come in a wider integer type are looked over (the device is waited
+    for) and narrowed here, once."""
 
     def __init__(self, codes, scales, row_scale=None, fmt="block32"):
         lead, rows, K = codes.shape[:-2], codes.shape[-2], 2 * codes.shape[-1]
@@ -152,7 +153,10 @@ class MXTensor:
         if (row_scale is not None) != (fmt == "block16") or (
                 row_scale is not None and row_scale.shape != codes.shape[:-1]):
             raise ValueError("block16 has one scale a row, block32 none")
-        if codes.dtype != torch.uint8 and not codes.is_floating_point():
+        if codes.dtype in (torch.int16, torch.int32, torch.int64):
+            lo, hi = torch.stack(torch.aminmax(codes)).tolist() if codes.numel() else (0, 0)
+            if lo < 0 or hi > 255:
+                raise ValueError("code bytes are 0 to 255, got %d to %d" % (lo, hi))
             codes = codes.to(torch.uint8).contiguous()
         _on(codes, torch.uint8, codes.device, "codes")
         _on(scales, torch.uint8, codes.device, "scales")

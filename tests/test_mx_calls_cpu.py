@@ -44,3 +44,23 @@ def test_results_are_recorded_on_the_callers_stream(fake, recorded, name):  # no
     call(None)
     call(FakeStream(HERE, fake.log))
     assert not recorded
+
+
+@pytest.mark.parametrize("bad", [256, -1, 1 << 32])
+@pytest.mark.parametrize("dtype", [torch.int16, torch.int32, torch.int64])
+def test_codes_that_are_no_bytes_are_refused(bad, dtype):
+    w = tensor(8, 64)
+    codes = torch.arange(256).view(8, 32).to(dtype)
+    assert torch.equal(mx.MXTensor(codes, w.scales).codes.to(dtype), codes)
+    if bad <= torch.iinfo(dtype).max:
+        codes[3, 5] = bad
+        with pytest.raises(ValueError, match="0 to 255"):
+            mx.MXTensor(codes, w.scales)
+    assert mx.MXTensor(codes[:0], w.scales[:0]).rows == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.int8, torch.bool, torch.complex64])
+def test_codes_of_other_types_are_refused(dtype):
+    w = tensor(8, 64)
+    with pytest.raises(ValueError, match="uint8"):
+        mx.MXTensor(w.codes.to(dtype), w.scales)
