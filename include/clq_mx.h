@@ -171,7 +171,7 @@ clq_status clq_mx_quantize_rows(const void* X, clq_dtype dtype, const void* plan
 /*
  * out[t] = sum_j weights[t][j] Y[rows[t][j]] over the places with rows >= 0, in
  * the order of j, in fp32.  Y: device [R][D] of `dtype`, D % 8 == 0, D <= 2^24; out:
- * [T][D].
+ * [T][D]; T and k below 2^30.
  */
 clq_status clq_mx_combine(const void* Y, clq_dtype dtype, const int32_t* rows,
                           const float* weights, int32_t T, int32_t k, int32_t D, int32_t R,

@@ -283,7 +283,7 @@ clq_status clq_mx_combine(const void* Y, clq_dtype dtype, const int32_t* rows,
                           const float* weights, int32_t T, int32_t k, int32_t D, int32_t R,
                           void* out, void* stream) {
   if (!valid_dtype(dtype) || T < 0 || k < 1 || R < 0) return CLQ_ERR_INVALID_ARG;
-  if (D < 8 || D % 8 != 0 || D > (1 << 24)) return CLQ_ERR_SHAPE;
+  if (D < 8 || D % 8 != 0 || D > (1 << 24) || T > kMaxRows || k > kMaxRows) return CLQ_ERR_SHAPE;
   if (T == 0) return CLQ_OK;
   if (Y == nullptr || rows == nullptr || weights == nullptr || out == nullptr)
     return CLQ_ERR_INVALID_ARG;

@@ -3,7 +3,7 @@ caller's stream, and what calls refuse."""
 import pytest
 import torch
 
-from paper_2509_24416_gb300 import clq, mx
+from paper_2509_24416_gb300 import build, clq, mx
 from test_streams_cpu import HERE, FakeStream, fake  # noqa: F401
 from test_mx_cpu import tensor
 
@@ -64,3 +64,12 @@ def test_codes_of_other_types_are_refused(dtype):
     w = tensor(8, 64)
     with pytest.raises(ValueError, match="uint8"):
         mx.MXTensor(w.codes.to(dtype), w.scales)
+
+
+P = 1 << 20  # a 16-byte aligned "device" address that nothing reads
+
+
+@pytest.mark.parametrize("T,k", [(1 << 30, 1), ((1 << 31) - 1, 1), (1, 1 << 30), (1, (1 << 31) - 1)])
+def test_combine_refuses_what_its_indices_do_not_hold(T, k):
+    build.build()
+    assert mx.clq_mx_combine(P, 0, P, P, T, k, 8, 8, P, None) == 2
