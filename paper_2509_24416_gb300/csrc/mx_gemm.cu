@@ -1,4 +1,4 @@
-// Launch of the microscaled product (mx_gemm.cuh): tensor maps and tile choice.
+// Launch of the microscaled product (mx_gemm.cuh): tensor maps.
 #include "mx_gemm.cuh"
 
 namespace clq {
@@ -17,63 +17,18 @@ bool scales_map(CUtensorMap* m, const uint8_t* p, int64_t chunks, int sc) {
                        static_cast<uint64_t>(chunks), 128, sc, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-// The tile of a product whose rows are `rows` for each of `matrices` matrices: the CTAs or
-// pairs go ceil(tiles / units) rounds; a round takes its K steps and the part of an epilogue
-// that the next round's MMAs do not cover, and the last epilogue and the launch come on top.
-// The times are fitted to 112 products of 33 .. 8192 rows (step: us for 256 codes; epilogue:
-// us a tile); the rule is within 10 % of the best of the five on all but six of them (18 % off at most).  Examples,
-// us at 64 / 128 / 128 in pairs / 256 / 256 in pairs: 64 x 1152 -> 3456 3.8 / 4.1 / 4.1 / 5.1 /
-// 4.8, 2048 x 4608 -> 1152 10.4 / 7.4 / 10.3 / 11.0 / 9.8, 4096 x 4608 -> 1152 18.4 / 11.7 /
-// 13.9 / 11.2 / 15.3, 8192 x 4096 -> 8192 190 / 114 / 91 / 110 / 83.
-TileShape pick_tile(int rows, int matrices, int N, int K, int sms, bool grouped) {
-  if (rows <= 32) return {32, 1};
-  struct Option {
-    TileShape t;
-    double step, epilogue;
-    bool plan;  // a plan has such tiles
-  };
-  const Option options[] = {{{64, 1}, 0.22, 0.75, false},
-                            {{128, 1}, 0.26, 1.03, true},
-                            {{128, 2}, 0.21, 1.03, false},
-                            {{256, 1}, 0.48, 1.8, false},
-                            {{256, 2}, 0.36, 1.8, true}};
-  TileShape best{128, 1};
-  double least = 1e300;
-  for (const Option& o : options) {
-    if (grouped && !o.plan) continue;
-    const int64_t tiles = static_cast<int64_t>(matrices) * ((rows + o.t.nt - 1) / o.t.nt) *
-                          ((N + TN * o.t.cg - 1) / (TN * o.t.cg));
-    const int64_t units = sms / o.t.cg;
-    const double cost = ((tiles + units - 1) / units) *
-                            ((K + KC - 1) / KC * o.step + 0.35 * o.epilogue) +
-                        o.epilogue;
-    if (cost < least) {
-      least = cost;
-      best = o.t;
-    }
-  }
-  return best;
-}
-
 }  // namespace
 
 cudaError_t launch_gemm(const uint8_t* Xq, const uint8_t* Xs, const uint8_t* Wq,
                         const uint8_t* Ws, const GemmArgs& args, int fmt, int dtype,
                         const void* plan, const PlanLayout* pl, int T, int k, cudaStream_t st) {
-  const int64_t picks = static_cast<int64_t>(T) * k;
   const int sms = sm_count();
   if (sms <= 0) return cudaErrorInvalidDevice;
   GemmArgs g = args;
   const bool grouped = plan != nullptr;
   const int64_t blocks = (g.x_rows + kRowBlock - 1) / kRowBlock;
-  // A plan's rows are taken as evenly spread over the matrices that have any; T rows at most
-  // meet one of them.
-  const int64_t spread = std::max<int64_t>(1, std::min<int64_t>(g.experts, picks));
-  const TileShape t =
-      grouped ? (T <= 32 ? TileShape{32, 1}
-                         : pick_tile(std::max(33, static_cast<int>((picks + spread - 1) / spread)),
-                                     static_cast<int>(spread), g.N, g.K, sms, true))
-              : pick_tile(g.M, 1, g.N, g.K, sms, false);
+  const TileShape t = grouped ? pick_grouped_tile(T, k, g.experts, g.N, g.K, sms)
+                              : pick_tile(g.M, 1, g.N, g.K, sms, false);
   const int nt = t.nt, cg = t.cg;
   if (grouped) {
     const uint8_t* p = static_cast<const uint8_t*>(plan);

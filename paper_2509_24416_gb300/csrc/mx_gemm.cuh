@@ -20,6 +20,7 @@
 #include "gemm_common.cuh"
 #include "mx_device.cuh"
 #include "mx_kernels.h"
+#include "mx_tiles.h"
 
 namespace clq {
 namespace mx {
@@ -27,8 +28,6 @@ namespace mx {
 using gemm::EPI_BYTES;
 using gemm::EPI_COLS;
 
-constexpr int TN = 128;   // output channels a CTA
-constexpr int KC = 256;   // codes of a K step: one 128-byte row
 constexpr int WARP_TMA = 4;
 constexpr int WARP_MMA = 5;
 // Eight: with sixteen the registers left to each spill (32768 x 4096 -> 8192 in blocks of 16
@@ -647,11 +646,6 @@ cudaError_t launch_gemm_t(const GemmMaps& m, const GemmArgs& g, int use_tma_stor
   return launch_cluster_pdl(k, grid, CG, THREADS, smem, st, m.W, m.X, m.SW, m.SX, m.Y, g,
                             use_tma_store);
 }
-
-// A tile: `nt` rows of X by 128 cg channels.
-struct TileShape {
-  int nt, cg;
-};
 
 // Instantiated for each output type and format in mx_gemm_*.cu.  A plan's tiles have up to
 // 128 or 256 rows; the epilogues that quantize go with them in blocks of 32.

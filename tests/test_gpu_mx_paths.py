@@ -3,6 +3,8 @@ test_gpu_mx.py do not reach, against their definitions in 64 bits (mx_utils)."""
 import pytest
 import torch
 
+import mx_tiles as tiles
+import mx_utils as ref
 from paper_2509_24416_gb300 import clq, mx
 
 pytestmark = pytest.mark.gpu
@@ -108,3 +110,131 @@ def test_product_right_behind_its_plan(T, k, E, N, K):
             assert plan(t) == 0 and product(t) == 0
         for t in turns:
             assert torch.equal(t[3], t[1]) and torch.equal(t[4][t[1].flatten().long()], t[5])
+
+
+# ------------------------------------------------------- every tile of the product --
+@pytest.fixture(scope="module")
+def picks(tmp_path_factory):
+    return tiles.library(tmp_path_factory.mktemp("tiles"))
+
+
+def sms():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def exact_tensor(g, rows, K, fmt, stack=(), low=0):
+    """Random codes; block scales of 2^low and twice that, row scales of 0.5, 1 and 2, so that sums
+    of products are exact in fp32.  The scales of rows past the last one, which nothing may use,
+    are NaN; those of blocks past the last one 0."""
+    lead = tuple(stack)
+    codes = torch.randint(0, 256, lead + (rows, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+    one, step, nan = (127 + low, 1, 255) if fmt == "block32" else (56 + 8 * low, 8, 127)
+    shape = mx.scale_shape(rows, K, fmt)
+    scales = (one + step * torch.randint(0, 2, lead + shape, generator=g, device=DEV)).to(torch.uint8)
+    i, c, r, j, q = (torch.arange(n, device=DEV) for n in shape)
+    row = 128 * i[:, None, None, None, None] + 32 * j[None, None, None, :, None] + r[None, None, :, None, None]
+    scales = torch.where(row < rows, scales, nan)
+    block = 4 * c[None, :, None, None, None] + q
+    scales = torch.where(block < K // ref.BLOCK[fmt], scales, 0).to(torch.uint8).contiguous()
+    rs = 2.0 ** torch.randint(-1, 2, lead + (rows,), generator=g, device=DEV) if fmt == "block16" else None
+    return mx.MXTensor(codes, scales, rs, fmt)
+
+
+def part(q, i):
+    """Matrix i of a stack."""
+    return mx.MXTensor(q.codes[i], q.scales[i], None if q.row_scale is None else q.row_scale[i], q.fmt)
+
+
+def values64(q):
+    grid = torch.tensor(list(ref.GRID) + list(-ref.GRID), dtype=torch.float64, device=DEV)
+    v = grid[torch.stack((q.codes & 15, q.codes >> 4), 2).view(q.rows, q.K).long()]
+    r, blk = torch.arange(q.rows, device=DEV)[:, None], torch.arange(q.K // ref.BLOCK[q.fmt], device=DEV)[None, :]
+    byte = q.scales[r // 128, blk // 4, r % 32, r % 128 // 32, blk % 4]
+    s = torch.exp2(byte.double() - 127) if q.fmt == "block32" else byte.view(torch.float8_e4m3fn).double()
+    if q.row_scale is not None:
+        s = s * q.row_scale.double()[:, None]
+    return v * s.repeat_interleave(ref.BLOCK[q.fmt], 1)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K,N,tile", tiles.DENSE)
+def test_linear_exact_in_every_tile(picks, fmt, M, K, N, tile):
+    """Sums that fp32 holds: at most 36 * 4 * 8192 of multiples of 1 / 4, and powers of two and a bias of
+    quarters on top."""
+    if sms() == 152:
+        assert tiles.dense(picks, M, N, K) == tile
+    g = gen(M + N)
+    dtype = F16 if (M + K) % 3 else BF16
+    x, w = exact_tensor(g, M, K, fmt), exact_tensor(g, N, K, fmt)
+    bias = (torch.randint(-64, 65, (N,), generator=g, device=DEV) / 4).to(dtype)
+    want = values64(x) @ values64(w).t() / 4 + bias.double()
+    assert torch.equal(want.float().double(), want)
+    want = want.float().to(dtype)
+    for _ in range(3):
+        assert torch.equal(mx.linear(x, w, bias, 4, dtype), want)
+
+
+def uneven_routing(g, T, k, E):
+    """Experts that get from few tokens to nearly all of them; some places without an expert."""
+    keys = torch.rand((T, E), generator=g, device=DEV) * torch.linspace(0.4, 1, E, device=DEV)
+    experts = keys.argsort(1, descending=True)[:, :k].to(torch.int32)
+    experts[torch.rand((T, k), generator=g, device=DEV) < 0.02] = -1
+    return mx.Routing(experts.contiguous(), torch.ones((T, k), device=DEV), E)
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("T,k,E,N,K,tile", tiles.GROUPED)
+def test_grouped_product_exact_in_every_tile(picks, fmt, T, k, E, N, K, tile):
+    if sms() == 152:
+        assert tiles.grouped(picks, T, k, E, N, K) == tile
+    g = gen(T + N)
+    dtype = F16 if T % 3 else BF16
+    r = uneven_routing(g, T, k, E)
+    rows, space, R = mx.plan(r)
+    x, w = exact_tensor(g, R, K, fmt), exact_tensor(g, N, K, fmt, (E,))
+    bias = (torch.randint(-64, 65, (E, N), generator=g, device=DEV) / 4).to(dtype)
+    for turn in range(3):
+        Y = torch.full((R, N), 7.0, dtype=dtype, device=DEV)
+        assert mx.clq_mx_grouped_linear(P(x.codes), P(x.scales), P(x.row_scale), P(space), P(w.codes), P(w.scales),
+                                        P(w.row_scale), P(bias), T, k, E, N, K, 4, mx.FORMATS[fmt], mx.DTYPES[dtype], P(Y),
+                                        stream()) == 0
+        xv = values64(x) if turn == 0 else xv
+        for e in range(E):
+            mine = rows[r.experts == e].long()  # none, for some of 20 tokens' experts
+            want = xv[mine] @ values64(part(w, e)).t() / 4 + bias[e].double()
+            assert torch.equal(Y[mine], want.float().to(dtype)), (turn, e)
+
+
+@pytest.mark.parametrize("act", ["swiglu", "gelu", None])
+@pytest.mark.parametrize("T,k,E,N,K,tile", tiles.GROUPED)
+def test_fused_activation_in_every_tile(picks, act, T, k, E, N, K, tile):
+    """The product that quantizes its output against the product (exact, above), then the
+    quantization: one activation function serves both, so the bytes are the same."""
+    N = N // 64 * 64 if act == "swiglu" else N
+    if sms() == 152:
+        assert tiles.grouped(picks, T, k, E, N, K) == tile
+    F = N // 2 if act == "swiglu" else N
+    g = gen(T + N)
+    dtype = F16 if T % 3 else BF16
+    r = uneven_routing(g, T, k, E)
+    rows, space, R = mx.plan(r)
+    # sums of the order of 1
+    x, w = exact_tensor(g, R, K, "block32", low=-4), exact_tensor(g, N, K, "block32", (E,), low=-5)
+    bias = (torch.randint(-8, 9, (E, N), generator=g, device=DEV) / 4).to(dtype)
+    dt = mx.DTYPES[dtype]
+    Y = torch.zeros((R, N), dtype=dtype, device=DEV)
+    assert mx.clq_mx_grouped_linear(P(x.codes), P(x.scales), None, P(space), P(w.codes), P(w.scales), None, P(bias), T, k, E, N,
+                                    K, 1, 0, dt, P(Y), stream()) == 0
+    a = [torch.zeros_like(t) for t in mx._empty(R, F, "block32", DEV)[:2]]
+    assert mx.clq_mx_quantize_rows(P(Y), dt, P(space), T, k, E, F, N, mx.ACTS[act], 0, P(a[0]), P(a[1]), None, stream()) == 0
+    used = rows[rows >= 0].long()
+    want = values64(mx.MXTensor(*a))[used]
+    assert 0.01 < want.abs().mean() < 100
+    for _ in range(3):
+        f = [torch.full_like(t, 99) for t in a]
+        assert mx.clq_mx_grouped_linear_act(P(x.codes), P(x.scales), P(space), P(w.codes), P(w.scales), P(bias), T, k, E, N, K,
+                                            1, dt, mx.ACTS[act], P(f[0]), P(f[1]), stream()) == 0
+        assert torch.equal(f[0][used], a[0][used])
+        blocks = 4 * -(-F // 128)
+        at = used.cpu().numpy()
+        assert (ref.scale_bytes(f[1], R, blocks)[at] == ref.scale_bytes(a[1], R, blocks)[at]).all()

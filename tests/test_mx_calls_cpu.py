@@ -1,8 +1,11 @@
 """CPU-only checks of the microscaled calls: what a call with an explicit stream hands back to the
 caller's stream, and what calls refuse."""
+import random
+
 import pytest
 import torch
 
+import mx_tiles as tiles
 from paper_2509_24416_gb300 import build, clq, mx
 from test_streams_cpu import HERE, FakeStream, fake  # noqa: F401
 from test_mx_cpu import tensor
@@ -73,3 +76,19 @@ P = 1 << 20  # a 16-byte aligned "device" address that nothing reads
 def test_combine_refuses_what_its_indices_do_not_hold(T, k):
     build.build()
     assert mx.clq_mx_combine(P, 0, P, P, T, k, 8, 8, P, None) == 2
+
+
+def test_shapes_of_the_tests_take_every_tile(tmp_path):
+    lib = tiles.library(tmp_path)
+    for M, K, N, tile in tiles.DENSE:
+        assert tiles.dense(lib, M, N, K) == tile, (M, K, N)
+    for T, k, E, N, K, tile in tiles.GROUPED:
+        assert tiles.grouped(lib, T, k, E, N, K) == tile, (T, k, E, N, K)
+    # no shape takes another one
+    rng = random.Random(5)
+    log = lambda lo, hi: int(lo * (hi / lo) ** rng.random())
+    seen = {tiles.dense(lib, log(1, 40000), log(1, 20000), 32 * log(1, 512)) for _ in range(20000)}
+    assert seen == {t[-1] for t in tiles.DENSE}
+    seen = {tiles.grouped(lib, log(1, 40000), rng.choice((1, 2, 4, 8)), log(8, 512), log(1, 8000), 32 * log(1, 512))
+            for _ in range(20000)}
+    assert seen == {t[-1] for t in tiles.GROUPED}
