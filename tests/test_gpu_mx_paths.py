@@ -238,3 +238,39 @@ def test_fused_activation_in_every_tile(picks, act, T, k, E, N, K, tile):
         blocks = 4 * -(-F // 128)
         at = used.cpu().numpy()
         assert (ref.scale_bytes(f[1], R, blocks)[at] == ref.scale_bytes(a[1], R, blocks)[at]).all()
+
+
+# ------------------------------------------------------------------------ routing --
+# E, groups: groups of a power of two from 32 on, of another multiple of 32, of a power of two
+# below 32, of any other size
+GROUPS = [(64, 2), (128, 2), (256, 4), (256, 2), (512, 2), (512, 4), (512, 16), (320, 5), (256, 8),
+          (192, 2), (384, 4), (320, 2), (448, 2), (288, 3),
+          (32, 32), (64, 32), (64, 16), (256, 32), (256, 16), (60, 15), (24, 3),
+          (300, 3), (96, 2), (144, 3), (45, 15), (288, 32), (33, 3), (500, 20)]
+
+
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("E,groups", GROUPS)
+def test_route_groups_of_every_size(E, groups, group_top):
+    g = gen(E + groups)
+    T, size = 96, E // groups
+    for turn, (scoring, k) in enumerate((("softmax", 1), ("sigmoid", 4), ("softmax", 6), ("sigmoid", 8), ("softmax", 9), ("sigmoid", 32))):
+        k = min(k, E)
+        top_groups = max(1, groups // 2) if turn % 2 else max(1, groups - 1)
+        L = torch.randn((T, E), generator=g, device=DEV)
+        if turn >= 4:  # many equal scores
+            L = L.round()
+        L[:16] = torch.where(torch.rand((16, E), generator=g, device=DEV) < 0.5, L[:16], -float("inf"))
+        by = L.view(T, groups, size)
+        by[16:24, 0] = -float("inf")  # no expert of a group
+        by[24:32, -1, 1:] = -float("inf")  # one
+        L[32:36] = -float("inf")
+        bal = 0.1 * torch.randn(E, generator=g, device=DEV) if turn in (1, 2) else None
+        r = mx.route(L, k, scoring, bal, groups, top_groups, group_top)
+        experts, weights, margin = ref.routing(L.cpu().double().numpy(), None if bal is None else bal.cpu().double().numpy(), k, scoring,
+                                               groups, top_groups, group_top)
+        # as in test_gpu_mx.py: fp32 scores are within 2^-20 of the exact ones, equal ones tie
+        clear = (margin > 2.0 ** -20) | (margin == 0)
+        assert clear.mean() > 0.9
+        assert (r.experts.cpu().numpy()[clear] == experts[clear]).all(), turn
+        assert abs(r.weights.cpu().double().numpy()[clear] - weights[clear]).max() <= 1e-5
