@@ -274,3 +274,150 @@ def test_route_groups_of_every_size(E, groups, group_top):
         assert clear.mean() > 0.9
         assert (r.experts.cpu().numpy()[clear] == experts[clear]).all(), turn
         assert abs(r.weights.cpu().double().numpy()[clear] - weights[clear]).max() <= 1e-5
+
+
+# -------------------------------------------------- quantization into chosen rows --
+def offset(t, nbytes):
+    """A copy of t that starts `nbytes` behind a 256-byte boundary."""
+    raw = torch.empty(t.numel() * t.element_size() + 256, dtype=torch.uint8, device=DEV)
+    at = -raw.data_ptr() % 256 + nbytes
+    out = raw[at:at + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+    out.copy_(t)
+    return out
+
+
+def quantize_to(X, fmt, perm, b, rows, R, codes_at=0):
+    """clq_mx_quantize into R rows, those of `rows` [M, k]; every byte elsewhere is 0xAB."""
+    M, K = X.shape
+    out = [None if t is None else t.view(torch.uint8).fill_(0xAB).view(t.dtype) for t in mx._empty(R, K, fmt, DEV)]
+    if codes_at:
+        out[0] = offset(out[0], codes_at)
+    assert mx.clq_mx_quantize(P(X), mx.DTYPES[X.dtype], M, K, X.stride(0), P(perm), b, 0, mx.FORMATS[fmt], *map(P, out), P(rows),
+                              rows.shape[1], R, stream()) == 0
+    return out
+
+
+def check_rows(out, want, to, R, fmt):
+    """Row to[i] of `out` is row i of the MXTensor `want`, and no other row was written."""
+    to = to.long()
+    blocks = want.K // ref.BLOCK[fmt]
+    padded = 4 * -(-blocks // 4)
+    assert torch.equal(out[0][to], want.codes)
+    got, expect = ref.scale_bytes(out[1], R, padded), ref.scale_bytes(want.scales, want.rows, padded)
+    assert (got[to.cpu().numpy()] == expect).all()
+    rest = torch.ones(R, dtype=torch.bool, device=DEV)
+    rest[to] = False
+    assert (out[0][rest] == 0xAB).all() and (got[rest.cpu().numpy()] == 0xAB).all()
+    if fmt == "block16":
+        bits = out[2].view(torch.int32)
+        assert torch.equal(out[2][to].nan_to_num(-1), want.row_scale.nan_to_num(-1))
+        assert (bits[rest] == bits.new_tensor([-0x54545455])).all()
+
+
+# the last one of each group is far below the threshold of the kernel for many rows
+INTO_ROWS = [(6601, 1152, 64), (6601, 1152, 128), (14007, 512, 64), (12001, 704, 64), (9001, 640, 128), (2500, 4608, 128), (120, 1152, 64)]
+
+
+@pytest.mark.parametrize("fmt", ["block32", "block16"])
+@pytest.mark.parametrize("M,K,b", INTO_ROWS)
+def test_quantize_into_rows(fmt, M, K, b):
+    """Codes, scales and row scales of rows that go to one, two or no other rows, in both kernels,
+    with a swap vector off a 16-byte and codes off a 32-byte boundary."""
+    g = gen(M + K)
+    X = torch.randn((M, K), generator=g, device=DEV).to(BF16)
+    X[M // 3, 5], X[M // 2, 3], X[M // 5] = float("inf"), float("nan"), 0
+    perm = torch.randperm(K, generator=g, device=DEV).to(torch.int32)
+    step = 128 * max(1, 60000 // K // 128)  # parts that take the kernel for few rows
+    parts = [mx.quantize(X[i:i + step], fmt, perm, b) for i in range(0, M, step)]
+    blocks = K // ref.BLOCK[fmt]
+    # the parts are whole blocks of 128 rows, so their scale arrays go end to end
+    want = mx.MXTensor(torch.cat([p.codes for p in parts]), torch.cat([p.scales for p in parts]),
+                       torch.cat([p.row_scale for p in parts]) if fmt == "block16" else None, fmt)
+    R = 2 * M + 5
+    places = torch.randperm(R, generator=g, device=DEV)[:2 * M].to(torch.int32).view(M, 2).contiguous()
+    places[1::3, 0] = -1
+    places[2::5, 1] = -1
+    at, which = places.flatten(), torch.arange(M, device=DEV).repeat_interleave(2)
+    live = at >= 0
+    picked = which[live]
+    scales = torch.from_numpy(ref.scale_bytes(want.scales, M, 4 * -(-blocks // 4))).to(DEV)[picked]
+    tiled = torch.zeros((-(-len(picked) // 128) * 128, scales.shape[1]), dtype=torch.uint8, device=DEV)
+    tiled[:len(picked)] = scales
+    tiled = tiled.view(-1, 4, 32, scales.shape[1] // 4, 4).permute(0, 3, 2, 1, 4).contiguous()
+    rows = mx.MXTensor(want.codes[picked].contiguous(), tiled, want.row_scale[picked] if fmt == "block16" else None, fmt)
+    for codes_at, perm_at in ((0, 0), (16, 4)):
+        out = quantize_to(X, fmt, offset(perm, perm_at), b, places, R, codes_at)
+        check_rows(out, rows, at[live], R, fmt)
+
+
+@pytest.mark.parametrize("M,K,b", [(6601, 1152, 64), (6601, 1152, 128), (40, 1152, 64)])
+def test_quantize_reports_indices_out_of_range(M, K, b):
+    """A row index past the last one is not written, an element of the swap vector that is none reads
+    element 0; both are reported."""
+    g = gen(M)
+    X = torch.randn((M, K), generator=g, device=DEV).to(F16)
+    perm = torch.randperm(K, generator=g, device=DEV).to(torch.int32)
+    rows = torch.arange(M, device=DEV).to(torch.int32)[:, None].contiguous()
+    want = quantize_to(X, "block16", perm, b, rows, M)
+    torch.cuda.synchronize()
+    assert clq.device_status() == 0
+    bad = rows.clone()
+    bad[M // 2], bad[M - 1] = M, 2 ** 31 - 1
+    out = quantize_to(X, "block16", perm, b, bad, M)
+    torch.cuda.synchronize()
+    assert clq.device_status() == 7
+    keep = torch.ones(M, dtype=torch.bool, device=DEV)
+    keep[M // 2] = keep[M - 1] = False
+    for o, w in zip((out[0], out[2]), (want[0], want[2])):
+        assert torch.equal(o[keep], w[keep])
+    assert (out[0][~keep] == 0xAB).all()
+    for value in (K, -1, 2 ** 31 - 1, -2 ** 31):
+        broken, zero = perm.clone(), perm.clone()
+        broken[K // 2 + 1], zero[K // 2 + 1] = value, 0
+        got = quantize_to(X, "block16", broken, b, rows, M)
+        torch.cuda.synchronize()
+        assert clq.device_status() == 7
+        expect = quantize_to(X, "block16", zero, b, rows, M)
+        assert torch.equal(got[0], expect[0]) and torch.equal(got[2], expect[2])
+
+
+def test_combine_reports_rows_out_of_range():
+    """A row past the last one adds nothing and is reported; one below 0 is a place without a row."""
+    g = gen(7)
+    Y = torch.randn((64, 48), generator=g, device=DEV).to(BF16)
+    rows = torch.randint(0, 64, (33, 3), generator=g, device=DEV).to(torch.int32)
+    w = torch.rand((33, 3), generator=g, device=DEV)
+    out = torch.empty((33, 48), dtype=BF16, device=DEV)
+    call = lambda r: mx.clq_mx_combine(P(Y), 1, P(r), P(w), 33, 3, 48, 64, P(out), stream())
+    none = rows.clone()
+    none[4, 1], none[20, 0], none[32, 2] = -1, -5, -1
+    assert call(none) == 0
+    want = out.clone()
+    assert clq.device_status() == 0
+    bad = none.clone()
+    bad[4, 1], bad[20, 0], bad[32, 2] = 64, 2 ** 31 - 1, 65
+    assert call(bad) == 0
+    torch.cuda.synchronize()
+    assert clq.device_status() == 7
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("T,k,E", [(16385, 2, 8), (16897, 3, 40), (40000, 8, 256), (70001, 2, 512)])
+def test_plan_of_many_tokens(T, k, E):
+    """More blocks of tokens than one turn of the prefix takes (128 of 128 tokens)."""
+    g = gen(T)
+    r = uneven_routing(g, T, k, E)
+    rows, space, R = mx.plan(r)
+    at = r.experts.long()
+    flat = at.flatten()
+    order = torch.sort(torch.where(flat < 0, E, flat), stable=True)
+    count = torch.bincount(flat[flat >= 0], minlength=E)
+    blocks = (count + 127) // 128 * 128
+    start = torch.cumsum(blocks, 0) - blocks
+    before = torch.cumsum(count, 0) - count
+    n = int(count.sum())
+    want = torch.full_like(flat, -1)
+    e = order.values[:n]
+    want[order.indices[:n]] = start[e] + torch.arange(n, device=DEV) - before[e]
+    assert torch.equal(rows.flatten().long(), want)
+    assert int(start[-1] + blocks[-1]) <= R
