@@ -39,8 +39,11 @@
  *            is 0; a row with an infinity or a NaN has s_row NaN (codes and
  *            scales 0).
  *   rn rounds to the nearest E2M1 value, ties to the even code, |.| > 6 to 6.
- * Every step is one IEEE fp32 operation in the order written; a value that is exactly 0
- * has code 0 (not 8, its negative).
+ * Every step, the swap and the rotation among them, is one IEEE fp32 operation in the
+ * order written, but for an activation (see clq_mx_act); a value that is exactly 0 has
+ * code 0 (not 8, its negative).
+ * VERSION.  clq_version counts the functions of clq.h alone; a library has those of this
+ * header if it has clq_mx_scale_bytes.
  */
 #ifndef CLQ_MX_H
 #define CLQ_MX_H
@@ -57,7 +60,10 @@ typedef int32_t clq_mx_format;
 
 #define CLQ_F32 2 /* logits of clq_mx_route only */
 
-/* What is applied to a row before the swap and the rotation, in fp32. */
+/* What is applied to a row before the swap and the rotation, in fp32: for every finite 16-bit
+ * input within 2^-21 |x| of the exact value (SWIGLU: 2^-21 |g u|, where that is a finite fp32
+ * number), wherever an activation is taken, so that a code may differ from the exact one's where
+ * a value lies that close to the middle of two, and so may the scale of a block (or a row). */
 typedef int32_t clq_mx_act;
 #define CLQ_MX_ACT_NONE 0
 #define CLQ_MX_ACT_GELU 1   /* 0.5 x (1 + erf(x / sqrt 2))                     */
@@ -92,7 +98,8 @@ clq_status clq_mx_dequantize(const uint8_t* codes, const uint8_t* scales, const 
 /*
  * Y[i][n] = out_dtype(sum_k x[i][k] w[n][k] / b + bias[n]), x and w the values of
  * two code arrays of one format, accumulated in fp32 (products of codes and scales
- * are exact).  Xq / Xs / s_x: codes, scales and (BLOCK16) row scales of M rows; Wq /
+ * are exact; BLOCK16's row scales and 1 / b are multiplied with one another first, in
+ * fp32, and the sum with that).  Xq / Xs / s_x: codes, scales and (BLOCK16) row scales of M rows; Wq /
  * Ws / s_w: of N; bias: device [N] of `dtype` or NULL; Y: device [M][N], 16-byte
  * aligned.  Codes and scales 16-byte, row scales 4-byte aligned.
  */
@@ -107,13 +114,15 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
  *   scoring 0: p = softmax(logits); 1: p = 1 / (1 + exp(-logit));
  *   c = p + balance (device fp32 [E] or NULL);
  *   groups > 1 (E % groups == 0): of the groups of E / groups neighbours the
- *   top_groups with the largest sum of their group_top (1 or 2) largest c stay;
+ *   top_groups with the largest sum of their group_top (1 or 2) largest c stay, ties to
+ *   the lowest; a masked expert's c counts as -infinity there, so that a group with one
+ *   among its group_top largest comes last;
  *   the k largest c, ties to the lowest index; weight = p, divided by the sum of the
  *   k if `renormalize`, times `scale`.
  * The softmax sums by halves (element i + element i + n / 2, n the power of two >= E,
  * missing ones 0, and so on), so its scores have one value.  A logit of
- * -infinity or NaN masks its expert; an infinity counts as the largest finite
- * value.  Places for which no expert is left hold expert -1 with weight 0.
+ * -infinity or NaN masks its expert, as does a c of those; an infinity counts as the
+ * largest finite value.  Places for which no expert is left hold expert -1 with weight 0.
  * experts: device int32 [T][k]; weights: device fp32 [T][k].
  */
 clq_status clq_mx_route(const void* logits, int32_t dtype, int32_t T, int32_t E, int32_t ld,
@@ -148,9 +157,9 @@ clq_status clq_mx_grouped_linear(const uint8_t* Xq, const uint8_t* Xs, const flo
 
 /*
  * The same product in blocks of 32, with its output as the next product's operand: h =
- * out_dtype(x w^T / b + bias) as clq_mx_grouped_linear would store it, then act(h), here
- * within 2^-20 |h| of its value (of |g u| for SWIGLU), quantized as by clq_mx_quantize, into Yq / Ys: codes and scales of clq_mx_plan_rows
- * rows of N codes (N / 2 for SWIGLU), N % 32 == 0 (64 for SWIGLU), at most 16384 codes.
+ * out_dtype(x w^T / b + bias) as clq_mx_grouped_linear would store it, then act(h), quantized
+ * as by clq_mx_quantize_rows, into Yq / Ys: codes and scales of clq_mx_plan_rows rows of N
+ * codes (N / 2 for SWIGLU), N % 32 == 0 (64 for SWIGLU), at most 16384 codes.
  */
 clq_status clq_mx_grouped_linear_act(const uint8_t* Xq, const uint8_t* Xs, const void* plan,
                                      const uint8_t* Wq, const uint8_t* Ws, const void* bias,
