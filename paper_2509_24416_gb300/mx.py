@@ -142,8 +142,8 @@ def _on_gpu(*tensors):
 class MXTensor:
     """Rows of E2M1 codes: ``codes`` uint8 [.., rows, K / 2], ``scales`` uint8 [.., *scale_shape]
     and, for "block16", ``row_scale`` fp32 [.., rows]; a leading dimension is a stack (of experts'
-    weights).  Code bytes that come in a wider integer type are looked over (the device is waited
-    for) and narrowed here, once."""
+    weights).  Code bytes that come in a wider integer type are narrowed here, once, after a look
+    at them (the device is waited for; under stream capture, which cannot wait, without)."""
 
     def __init__(self, codes, scales, row_scale=None, fmt="block32"):
         lead, rows, K = codes.shape[:-2], codes.shape[-2], 2 * codes.shape[-1]
@@ -154,9 +154,10 @@ class MXTensor:
                 row_scale is not None and row_scale.shape != codes.shape[:-1]):
             raise ValueError("block16 has one scale a row, block32 none")
         if codes.dtype in (torch.int16, torch.int32, torch.int64):
-            lo, hi = torch.stack(torch.aminmax(codes)).tolist() if codes.numel() else (0, 0)
-            if lo < 0 or hi > 255:
-                raise ValueError("code bytes are 0 to 255, got %d to %d" % (lo, hi))
+            if codes.numel() and not (codes.is_cuda and torch.cuda.is_current_stream_capturing()):
+                lo, hi = torch.stack(torch.aminmax(codes)).tolist()
+                if lo < 0 or hi > 255:
+                    raise ValueError("code bytes are 0 to 255, got %d to %d" % (lo, hi))
             codes = codes.to(torch.uint8).contiguous()
         _on(codes, torch.uint8, codes.device, "codes")
         _on(scales, torch.uint8, codes.device, "scales")

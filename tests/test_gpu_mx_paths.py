@@ -421,3 +421,22 @@ def test_plan_of_many_tokens(T, k, E):
     want[order.indices[:n]] = start[e] + torch.arange(n, device=DEV) - before[e]
     assert torch.equal(rows.flatten().long(), want)
     assert int(start[-1] + blocks[-1]) <= R
+
+
+def test_wider_codes_under_capture():
+    """Codes in a wider type are narrowed under stream capture too, where nothing can be read back."""
+    g = gen(11)
+    w = exact_tensor(g, 64, 128, "block32")
+    x = exact_tensor(g, 3, 128, "block32")
+    wide = w.codes.long()
+    want = mx.linear(x, w, dtype=F16)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = mx.linear(x, mx.MXTensor(wide, w.scales), dtype=F16)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    wide[5, 7] = -3
+    with pytest.raises(ValueError, match="0 to 255"):
+        mx.MXTensor(wide, w.scales)
