@@ -391,7 +391,8 @@ class MXExperts:
     @classmethod
     def from_weights(cls, W1, W2, fmt="block32", act="swiglu", perm=None, b=1, bias1=None,
                      bias2=None):
-        """From full-precision weights W1 [E, N1, K], W2 [E, N, F]."""
+        """From full-precision weights W1 [E, N1, K] (gated: its rows in the order that the class
+        takes, eight of the gate, eight of the up half), W2 [E, N, F]."""
         def stack(W, perm, b):
             q = [quantize(w, fmt, perm, b) for w in W]
             return MXTensor(torch.stack([t.codes for t in q]), torch.stack([t.scales for t in q]),
