@@ -218,10 +218,12 @@ __device__ __forceinline__ void post_tiles(Bars& bars, uint8_t* smem, const CUte
     tc_fence_after();
     const uint32_t acc = tmem + buf * (NT - C::OV) + (static_cast<uint32_t>(quarter * 32) << 16);
     // Of CTAs that share the tile, the first adds up what the others send it, in their order, and
-    // goes on; its operands' buffers take it as soon as its own MMAs are done.
+    // goes on; its operands' buffers take it as soon as its own MMAs are done.  Both barriers hand
+    // shared memory from one CTA to another, so both count at the cluster's scope.
     if (C::JOIN && split > 1) {
-      if (share == 0 && warp == 0 && lane > 0 && lane < split) mbar_arrive_cluster(cluster_addr(&bars.go, lane));
-      const bool there = mbar_wait_bounded(share == 0 ? &bars.joined : &bars.go, 0, abort, g.status, kWaitLimitNs);
+      if (share == 0 && warp == 0 && lane > 0 && lane < split)
+        mbar_arrive_cluster_release(cluster_addr(&bars.go, lane));
+      const bool there = mbar_wait_bounded<true>(share == 0 ? &bars.joined : &bars.go, 0, abort, g.status, kWaitLimitNs);
       if (!__all_sync(0xffffffffu, there)) break;
       if (share > 0) {
         const uint32_t bar = cluster_addr(&bars.joined, 0);

@@ -276,6 +276,50 @@ def test_shared_tiles_not_finite(at):
     assert Y[5].isnan().all() and Y.isnan().sum() == 300
 
 
+SHARED = [("block32_e4m3",) + s for s in SHARED8] + [(f,) + s for f in ("block32", "block16") for s in SHARED4]
+
+
+@pytest.mark.parametrize("fmt,M,K,N,tile", SHARED)
+def test_shared_tiles_of_every_format(fmt, M, K, N, tile):
+    """The same bits every time, beside other products, alone in a graph, and in the residual's place."""
+    g = gen(M + K)
+    x, w, bias = operands(g, M, K, N, fmt, F16, True)
+    R = rows_of(g, M, N, F16)
+    call = lambda **to: mx.linear(x, w, bias, dtype=F16, post="gelu", residual=R, **to)
+    first = call()
+    check(first, x, w, bias, 1, "gelu", R)
+    sides = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = [call(stream=s) for _ in range(20) for s in sides]
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, first) for y in got)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ys = [call() for _ in range(8)]  # each begins while the one before it ends
+    for _ in range(5):
+        for y in ys:
+            y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, first) for y in ys)
+    Y = R.clone()
+    assert mx.linear(x, w, bias, dtype=F16, Y=Y, post="gelu", residual=Y) is Y
+    assert torch.equal(Y, first)
+
+
+@pytest.mark.parametrize("fmt,M,K,N,tile", SHARED)
+def test_shared_tiles_not_finite_in_every_format(fmt, M, K, N, tile):
+    """A value that is not finite, met by the first CTA, one in between or the last, is its row's alone."""
+    g = gen(N)
+    w = mx.quantize(rows_of(g, N, K, BF16, 0.1), fmt)
+    for at in (0, K // 2, K - 1):
+        X = rows_of(g, M, K, BF16)
+        X[M // 2, at] = float("inf")
+        Y = mx.linear(mx.quantize(X, fmt), w, post="gelu")
+        assert Y[M // 2].isnan().all() and Y.isnan().sum() == N
+
+
+
 # ------------------------------------------------------------- the three in a row --
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [F16, BF16])
