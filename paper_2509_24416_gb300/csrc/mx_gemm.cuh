@@ -688,6 +688,9 @@ __global__ void __launch_bounds__((Cfg<FMT, NT, CG, EPI>::THREADS), 1)
     cluster_sync();
   else
     __syncthreads();
+  // On an abort: every CTA has sent what it sends by now, and that lands before this one exits.
+  if (C::JOIN && split > 1 && share == 0 && *abort != 0)
+    mbar_wait_bounded<true>(&bars.joined, 0, nullptr, nullptr, 10000000ull);
   if (warp == WARP_MMA) {
     tc_fence_after();
     tmem_dealloc<CG>(tmem, C::TMEM);
