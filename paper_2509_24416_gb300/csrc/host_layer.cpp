@@ -15,6 +15,8 @@
 // their C calls, rope that of rope.py.
 #include <Python.h>
 
+#include <cstring>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
@@ -172,6 +174,19 @@ bool rows_like(const at::Tensor* t, int64_t rows, int64_t columns, const at::Ten
 int32_t stride_of(const at::Tensor* t, int64_t rows, int64_t columns) {
   return t == nullptr ? 0 : static_cast<int32_t>(rows <= 1 ? columns : t->stride(0));
 }
+// The pairs of each axis of rotary positions (int32, handed over as bytes): none if they are not
+// those of `axes` axes and of `turns`, one 64-bit number each.
+struct Sections {
+  int32_t n[4] = {0, 0, 0, 0};
+  bool good = false;
+  Sections(PyObject* bytes, long axes, const at::Tensor* turns) {
+    if (axes < 1 || axes > 4 || !PyBytes_Check(bytes) || PyBytes_GET_SIZE(bytes) != 4 * axes || turns == nullptr ||
+        turns->scalar_type() != at::kLong || turns->dim() != 1 || !turns->is_contiguous())
+      return;
+    std::memcpy(n, PyBytes_AS_STRING(bytes), 4 * axes);
+    good = int64_t{n[0]} + n[1] + n[2] + n[3] == turns->numel();
+  }
+};
 PyObject* status_of(clq_status st, long where) { return PyLong_FromLong(st | (where << 8)); }
 // The interpreter's lock is given up while the C calls run: a full launch queue blocks them.
 struct Unlocked {
@@ -351,7 +366,7 @@ PyObject* mx_layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 }
 
 // mx_norm_linear(X, residual | None, weight | None, eps, fmt, perm | None, b, codes, scales,
-// row_scale | None, bias | None, post, positions | None, turns | None, host_sections (an address), axes, D,
+// row_scale | None, bias | None, post, positions | None, turns | None, pairs of each axis | None, axes, D,
 // pairs, heads) -> (Y, the sum | None), None or status | 256 * (0 norm, 1 product, 2 product with
 // what is behind it, 3 positions); the arrays of the layer's MXTensor.
 PyObject* mx_norm_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -362,7 +377,6 @@ PyObject* mx_norm_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
                    *wq = a.tensor(7), *ws = a.tensor(8), *wr = a.maybe(9), *bias = a.maybe(10),
                    *positions = a.maybe(12), *turns = a.maybe(13);
   const double eps = PyFloat_AsDouble(args[3]);
-  const void* sections = PyLong_AsVoidPtr(args[14]);
   if (PyErr_Occurred()) {
     PyErr_Clear();
     Py_RETURN_NONE;
@@ -372,6 +386,8 @@ PyObject* mx_norm_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (!a.plain || post < 0 || !rows16(X) || wq->dim() != 2 || wq->device() != X->device() ||
       (positions == nullptr) != (turns == nullptr))
     Py_RETURN_NONE;
+  const Sections sections(args[14], axes, turns);
+  if (positions != nullptr && !sections.good) Py_RETURN_NONE;
   const int64_t M = X->size(0), K = X->size(1), N = wq->size(0);
   const int64_t columns = post == CLQ_MX_ACT_SWIGLU ? N / 2 : N;
   if (M == 0 || K != codes_in(wq->size(1), fmt) || !dense(perm, at::kInt, K, *X) ||
@@ -410,7 +426,7 @@ PyObject* mx_norm_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (positions != nullptr) {
     st = unlocked(clq_rope, Y.data_ptr(), dt, m, static_cast<int32_t>(heads), static_cast<int32_t>(D), columns,
                   static_cast<int64_t>(D), data<int32_t>(positions), static_cast<int32_t>(positions->stride(0)),
-                  static_cast<int32_t>(axes), static_cast<const int32_t*>(sections),
+                  static_cast<int32_t>(axes), sections.n,
                   static_cast<const uint64_t*>(turns->data_ptr()), static_cast<clq_rope_pairs>(pairs), 0,
                   Y.data_ptr(), columns, static_cast<int64_t>(D), stream);
     if (st != CLQ_OK) return status_of(st, 3);
@@ -427,20 +443,16 @@ PyObject* mx_norm_linear(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// rope(x, positions, turns, host_sections (an address), axes, D, pairs, inverse, out | None) ->
+// rope(x, positions, turns, pairs of each axis, axes, D, pairs, inverse, out | None) ->
 // out, None or a status.
 PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
   if (nargs != 9) Py_RETURN_NONE;
   Args a{args};
   const at::Tensor *x = a.tensor(0), *positions = a.tensor(1), *turns = a.tensor(2), *out = a.maybe(8);
-  const void* sections = PyLong_AsVoidPtr(args[3]);
-  if (PyErr_Occurred()) {
-    PyErr_Clear();
-    Py_RETURN_NONE;
-  }
   const long axes = a.num(4), D = a.num(5), pairs = a.num(6), inverse = a.num(7);
-  if (!a.plain || !here(x) || x->dim() != 3 || x->size(2) != D || x->stride(2) != 1 ||
+  const Sections sections(args[3], axes, turns);
+  if (!a.plain || !sections.good || !here(x) || x->dim() != 3 || x->size(2) != D || x->stride(2) != 1 ||
       (x->scalar_type() != at::kHalf && x->scalar_type() != at::kBFloat16) ||
       x->size(0) > INT32_MAX || x->size(1) > INT32_MAX || positions->dim() != 2 ||
       positions->scalar_type() != at::kInt || positions->size(0) != x->size(0) ||
@@ -460,7 +472,7 @@ PyObject* rope(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const clq_status st = unlocked(clq_rope, x->data_ptr(), dtype_of(*x), static_cast<int32_t>(x->size(0)),
       static_cast<int32_t>(x->size(1)), static_cast<int32_t>(D), x->stride(0), x->stride(1),
       data<int32_t>(positions), static_cast<int32_t>(positions->stride(0)), static_cast<int32_t>(axes),
-      static_cast<const int32_t*>(sections), static_cast<const uint64_t*>(turns->data_ptr()),
+      sections.n, static_cast<const uint64_t*>(turns->data_ptr()),
       static_cast<clq_rope_pairs>(pairs), static_cast<int32_t>(inverse), out->data_ptr(), out->stride(0),
       out->stride(1), current_stream());
   if (st != CLQ_OK) return status_of(st, 0);

@@ -418,7 +418,7 @@ class MXNormLinear:
         lin = self.linear
         w, rope = lin.w, self.rope
         turned = (None, None, 0, 0, 0, 0, 0) if rope is None else (
-            positions, rope.turns, rope.address, rope.axes, rope.head_dim, rope.layout, self.heads)
+            positions, rope.turns, rope.section_pairs, rope.axes, rope.head_dim, rope.layout, self.heads)
         r = _native("mx_norm_linear", X, residual, self.weight, self.eps, FORMATS[w.fmt], lin.perm, lin.b,
                     w.codes, w.scales, w.row_scale, lin.bias, ACTS[self.post], *turned,
                     where=("clq_mx_rms_norm", "clq_mx_linear", "clq_mx_linear_post", "clq_rope"))

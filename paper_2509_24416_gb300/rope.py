@@ -6,6 +6,7 @@ width.  Every step runs in libclq.so.
 """
 import ctypes
 import fractions
+import struct
 
 import torch
 
@@ -81,8 +82,9 @@ class Rope:
         self.turns = torch.tensor([_turn(f) for f in freqs], dtype=torch.int64).to(device)
         if self.turns.is_cuda:  # whichever stream uses it first
             torch.cuda.current_stream(self.turns.device).synchronize()
-        self._sections = (ctypes.c_int32 * self.axes)(*(s // 2 for s in sections))
-        self.address, self.layout = ctypes.addressof(self._sections), PAIRS[pairs]
+        # int32 pairs of each axis, as bytes: a copy of this object has them too, wherever they lie
+        self.section_pairs = struct.pack("=%di" % self.axes, *(s // 2 for s in sections))
+        self.layout = PAIRS[pairs]
 
     def __call__(self, x, positions, out=None, inverse=False, stream=None):
         """x [T, H, head_dim] fp16 / bf16 with unit stride in a head (any strides of tokens and
@@ -94,7 +96,7 @@ class Rope:
         host = clq._host or clq._find_host()
         fn = getattr(host, "rope", None) if host else None
         if fn is not None:
-            r = fn(x, positions, self.turns, self.address, self.axes, self.head_dim, self.layout,
+            r = fn(x, positions, self.turns, self.section_pairs, self.axes, self.head_dim, self.layout,
                    int(bool(inverse)), out)
             if r is not None:
                 if type(r) is int:
@@ -113,9 +115,13 @@ class Rope:
         elif (out.shape != x.shape or out.dtype != x.dtype or out.stride(2) != 1
               or (T > 1 and out.stride(0) == 0) or (H > 1 and out.stride(1) == 0)):
             raise ValueError("out must be like x, with unit stride in a head and places of its own for each")
+        sections = (ctypes.c_int32 * self.axes).from_buffer_copy(self.section_pairs)
+        if self.turns.dtype != torch.int64 or tuple(self.turns.shape) != (sum(sections),) or not self.turns.is_contiguous():
+            raise ValueError("turns must be one contiguous int64 a pair, %d of them, got %s %s"
+                             % (sum(sections), self.turns.dtype, tuple(self.turns.shape)))
         _on_gpu(x, positions, out, self.turns)
         _check(clq_rope(_ptr(x), _dt(x), T, H, D, x.stride(0), x.stride(1), _ptr(positions),
-                        positions.stride(0), self.axes, self._sections, _ptr(self.turns),
+                        positions.stride(0), self.axes, sections, _ptr(self.turns),
                         self.layout, int(bool(inverse)), _ptr(out), out.stride(0),
                         out.stride(1), _stream(stream)), "clq_rope")
         return out

@@ -1,9 +1,13 @@
 """CPU-only checks of norm, product with what is behind it and rotary positions: declarations, refusals before any
 launch, the argument checks of the tensor helpers, streams, and the 64-bit fractions of a turn."""
+import copy
 import ctypes
+import gc
 import os
+import pickle
 import random
 import re
+import struct
 from fractions import Fraction
 
 import pytest
@@ -244,3 +248,48 @@ def test_streams_of_buffers_and_results(fake, monkeypatch, name):  # noqa: F811
         log.clear(), seen.clear()
         call(s)
         assert log and all(e[-1] == HERE for e in log) and not seen, log
+
+
+@pytest.mark.parametrize("how", ["deepcopy", "copy", "pickle"])
+def test_copies_of_positions(monkeypatch, lib, how):
+    """A copy whose original is gone hands over its own pairs of each axis, alone and in a layer."""
+    duplicate = {"deepcopy": copy.deepcopy, "copy": copy.copy, "pickle": lambda o: pickle.loads(pickle.dumps(o))}[how]
+    seen = []
+
+    class Host:
+        rope = staticmethod(lambda *a: seen.append((a[2], a[3], a[4])) or a[0])
+        mx_norm_linear = staticmethod(lambda *a: seen.append((a[13], a[14], a[15])) or (a[0], None))
+    monkeypatch.setattr(clq, "_host", Host)
+    first = mx.MXNormLinear(mx.MXLinear(tensor(128, 64)), rope=rope.Rope(64, (16, 24, 24), device="cpu"), heads=2)
+    turns = first.rope.turns.clone()
+    second = duplicate(first)
+    first = None
+    gc.collect()
+    spoil = [(ctypes.c_int32 * 3)(7, 7, 7) for _ in range(1000)]
+    X, positions = torch.zeros((4, 64), dtype=H), torch.zeros((4, 3), dtype=torch.int32)
+    second(X, positions=positions)
+    second.rope(X.view(4, 1, 64), positions)
+    third = rope.Rope(64, (16, 24, 24), device="cpu")
+    third = duplicate(third)
+    third(X.view(4, 1, 64), positions)
+    assert len(spoil) == 1000 and len(seen) == 3
+    for t, pairs, axes in seen:
+        assert axes == 3 and struct.unpack("=3i", pairs) == (8, 12, 12) and torch.equal(t, turns)
+    # and without the native form
+    monkeypatch.setattr(clq, "_host", None)
+    monkeypatch.setattr(clq, "_find_host", lambda: None)
+    monkeypatch.setattr(rope, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(rope, "_stream", lambda s: None)
+    monkeypatch.setattr(rope, "clq_rope", lambda *a: seen.append(list(a[10])) or 0)
+    third(X.view(4, 1, 64), positions)
+    assert seen[-1] == [8, 12, 12]
+
+
+@pytest.mark.parametrize("turns", [torch.zeros(31, dtype=torch.int64), torch.zeros(33, dtype=torch.int64),
+                                   torch.zeros(32, dtype=torch.int32), torch.zeros(64, dtype=torch.int64)[::2]])
+def test_frequencies_of_other_pairs_are_refused(monkeypatch, turns):
+    monkeypatch.setattr(rope, "_on_gpu", lambda *t: None)
+    r = rope.Rope(64, (16, 24, 24), device="cpu")
+    r.turns = turns
+    with pytest.raises(ValueError, match="turns"):
+        r(torch.zeros((4, 1, 64), dtype=H), torch.zeros((4, 3), dtype=torch.int32))
