@@ -121,7 +121,8 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
  * squares that fp32 does not hold is taken scaled, so every row of finite values has its norm;
  * a row with an infinity or a NaN has the values that the formula gives).  residual: device
  * [M][ldr] of `dtype` or NULL; sum: device [M][lds], receives h: with a residual only, and may
- * be X or the residual itself (same rows and stride).  weight: device [K] of `dtype` or NULL
+ * be X or the residual itself (same rows and stride); other rows or columns of them are refused,
+ * and ranges of addresses that meet where the strides differ.  weight: device [K] of `dtype` or NULL
  * (ones).  eps > 0.  X, residual, sum and weight 16-byte aligned, strides % 8 == 0.
  */
 clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K, int32_t ldx,
@@ -137,9 +138,9 @@ clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K,
  * stated at clq_mx_act.  SWIGLU: N % 16 == 0, channels 16 j .. + 7 are the gate and
  * 16 j + 8 .. + 15 the up half of columns 8 j .. + 7, Y and residual have N / 2 columns.
  * residual: device [M][ldr] of `dtype`, 2-byte aligned, any ldr >= its columns, or NULL; it may
- * be Y itself (ldr then Y's columns).  The order of a sum over k here, and in clq_mx_linear of
- * CLQ_MX_BLOCK32_E4M3, depends on M, N, K and on whether anything
- * stands behind the product (few rows share K out), not on the values or the call.
+ * be Y itself (ldr then Y's columns); one that meets Y otherwise is refused.  The order
+ * of a sum over k here, and in clq_mx_linear of CLQ_MX_BLOCK32_E4M3, depends on M, N, K and on
+ * whether anything stands behind the product (few rows share K out), not on the values or the call.
  */
 clq_status clq_mx_linear_post(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
                               const uint8_t* Wq, const uint8_t* Ws, const float* s_w,

@@ -35,7 +35,8 @@ typedef int32_t clq_rope_pairs;
  * x, out: device, `dtype` (fp16 / bf16); token t, head h, value d at
  * t token_stride + h head_stride + d (elements, not negative); out's
  * heads are apart, all of a token inside its stride or all of a head number inside theirs; out may
- * be x itself with the same strides, and does not overlap it otherwise.  T < 2^30 tokens of H
+ * be x itself with the same strides, and does not meet it otherwise (refused; where x has other strides
+ * than out, and not 0 instead, ranges of addresses that meet are).  T < 2^30 tokens of H
  * <= 65535 heads of D <= 4096 values.  positions: device int32, that of axis a of
  * token t at t ld_positions + a, any sign.  axes: 1 to 4; host_sections: host int32
  * [axes], pairs of each axis (0 or more), 1 <= P = their sum <= D / 2.  turns: device

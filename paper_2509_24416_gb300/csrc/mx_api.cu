@@ -6,6 +6,7 @@
 #include <cuda_runtime.h>
 
 #include "mx_kernels.h"
+#include "overlap.h"
 
 namespace {
 
@@ -16,6 +17,10 @@ bool valid_dtype(int d) { return d == CLQ_F16 || d == CLQ_BF16; }
 bool valid_format4(int f) { return f == CLQ_MX_BLOCK32 || f == CLQ_MX_BLOCK16; }
 bool valid_format(int f) { return valid_format4(f) || f == CLQ_MX_BLOCK32_E4M3; }
 bool valid_act(int a) { return a >= CLQ_MX_ACT_NONE && a <= CLQ_MX_ACT_SWIGLU; }
+// Rows of an output that meet other rows (or other places) of an input than their own.
+bool rows_overlap(const void* out, int64_t ld_out, const void* in, int64_t ld_in, int64_t rows, int64_t columns) {
+  return overlaps(out, {ld_out, 0}, in, {ld_in, 0}, {rows, 1}, columns);
+}
 constexpr int kMaxRows = (1 << 30) - 1;  // row indices and a grid's step beyond them fit an int
 bool valid_k(int K) { return K >= 32 && K <= 16384 && K % 32 == 0; }
 bool valid_b(int b, int K) { return b >= 1 && b <= 256 && (b & (b - 1)) == 0 && K % b == 0; }
@@ -191,6 +196,8 @@ clq_status clq_mx_linear_post(const uint8_t* Xq, const uint8_t* Xs, const float*
   if (residual != nullptr && ldr < (gated ? N / 2 : N)) return CLQ_ERR_SHAPE;
   if (!aligned(residual, 2)) return CLQ_ERR_ALIGN;
   if (residual != nullptr && residual == Y && M > 1 && ldr != (gated ? N / 2 : N)) return CLQ_ERR_INVALID_ARG;
+  if (residual != nullptr && Y != nullptr && aligned(Y, 2) && rows_overlap(Y, gated ? N / 2 : N, residual, ldr, M, gated ? N / 2 : N))
+    return CLQ_ERR_INVALID_ARG;
   return dense(Xq, Xs, s_x, Wq, Ws, s_w, bias, M, N, K, b, fmt, dtype,
                act != CLQ_MX_ACT_NONE || residual != nullptr, act, residual, ldr, Y, stream);
 }
@@ -213,6 +220,8 @@ clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K,
   if (!aligned(X, 16) || !aligned(residual, 16) || !aligned(sum, 16) || !aligned(weight, 16) ||
       !aligned(perm, 4))
     return CLQ_ERR_ALIGN;
+  if (both && (rows_overlap(sum, lds, X, ldx, M, K) || rows_overlap(sum, lds, residual, ldr, M, K)))
+    return CLQ_ERR_INVALID_ARG;
   clq_status st = check_codes(codes, scales, row_scale, fmt, 4);
   if (st != CLQ_OK) return st;
   mx::NormArgs a{};

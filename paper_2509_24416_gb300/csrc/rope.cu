@@ -16,6 +16,7 @@
 #include "../../include/clq_rope.h"
 #include "clq_device.cuh"
 #include "clq_kernels.h"
+#include "overlap.h"
 
 namespace clq {
 namespace rope {
@@ -239,6 +240,8 @@ extern "C" clq_status clq_rope(const void* x, clq_dtype dtype, int32_t T, int32_
     return CLQ_ERR_INVALID_ARG;
   if (!aligned(x, 2) || !aligned(out, 2) || !aligned(positions, 4) || !aligned(turns, 8))
     return CLQ_ERR_ALIGN;
+  if (overlaps(out, {out_token_stride, out_head_stride}, x, {token_stride, head_stride}, {T, H}, D))
+    return CLQ_ERR_INVALID_ARG;
   const clq_status st = device_check();
   if (st != CLQ_OK) return st;
   a.x = static_cast<const uint16_t*>(x);

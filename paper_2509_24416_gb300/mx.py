@@ -300,7 +300,8 @@ def linear(x, w, bias=None, b=1, dtype=torch.bfloat16, Y=None, stream=None, post
            residual=None):
     """x (MXTensor of M rows), w (of N rows) -> Y [M, N] = post(x w^T / b + bias) + residual, in fp32
     up to one rounding.  post "swiglu": of 16 channels 8 are the gate and 8 the up half, and Y and
-    the residual have N / 2 columns; see clq_mx_linear_post."""
+    the residual have N / 2 columns.  The residual may be Y, and does not meet it otherwise; see
+    clq_mx_linear_post."""
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, linear, x, w, bias, b, dtype, Y, None, post, residual)
     _pair(x, w)
@@ -334,7 +335,8 @@ def rms_norm(X, weight=None, residual=None, eps=1e-6, fmt="block32_e4m3", perm=N
              stream=None):
     """X [M, K] fp16 / bf16 -> MXTensor of norm(X) weight, swapped and rotated as in ``quantize``;
     with a residual [M, K] (MXTensor of norm(h), h), h = X + residual rounded to X's type.
-    ``out`` receives h (it may be X or the residual); see clq_mx_rms_norm."""
+    ``out`` receives h (it may be X or the residual, and does not meet them otherwise); see
+    clq_mx_rms_norm."""
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, rms_norm, X, weight, residual, eps, fmt, perm, b, out)
     f = _format(fmt)

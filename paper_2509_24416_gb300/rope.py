@@ -89,7 +89,7 @@ class Rope:
     def __call__(self, x, positions, out=None, inverse=False, stream=None):
         """x [T, H, head_dim] fp16 / bf16 with unit stride in a head (any strides of tokens and
         heads), positions int32 [T, axes] -> x turned, [T, H, head_dim]; ``out``: written there
-        (x itself: in place; heads that overlap one another are refused).  ``inverse`` turns back:
+        (x itself: in place; heads that overlap one another, or others of x, are refused).  ``inverse`` turns back:
         the gradient of x from that of the result."""
         if stream is not None and _elsewhere(stream):
             return _with_stream(stream, self, x, positions, out, inverse)

@@ -8,6 +8,7 @@ import pickle
 import random
 import re
 import struct
+import subprocess
 from fractions import Fraction
 
 import pytest
@@ -293,3 +294,83 @@ def test_frequencies_of_other_pairs_are_refused(monkeypatch, turns):
     r.turns = turns
     with pytest.raises(ValueError, match="turns"):
         r(torch.zeros((4, 1, 64), dtype=H), torch.zeros((4, 3), dtype=torch.int32))
+
+
+OVERLAP = """
+#include "overlap.h"
+extern "C" int overlap(int64_t out, const int64_t* so, int64_t in, const int64_t* si, const int64_t* n, int64_t D) {
+  const int64_t a[2] = {so[0], so[1]}, b[2] = {si[0], si[1]}, c[2] = {n[0], n[1]};
+  return clq::overlaps(reinterpret_cast<void*>(out), a, reinterpret_cast<void*>(in), b, c, D);
+}
+"""
+
+
+def test_overlap_against_sets(tmp_path):
+    """The check of outputs against inputs, place by place."""
+    so = str(tmp_path / "overlap.so")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", build.CSRC, "-x", "c++", "-", "-o", so],
+                       input=OVERLAP, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    fn = ctypes.CDLL(so).overlap
+    two = ctypes.c_int64 * 2
+    fn.argtypes = [ctypes.c_int64, two, ctypes.c_int64, two, two, ctypes.c_int64]
+    rng = random.Random(3)
+    places = lambda at, s, n, D: {at + i * s[0] + j * s[1] + c for i in range(n[0]) for j in range(n[1]) for c in range(D)}
+    seen = {(a, b): 0 for a in (True, False) for b in (True, False)}
+    for _ in range(60000):
+        n, D = [rng.randint(1, 4), rng.randint(1, 4)], rng.randint(1, 5)
+        inner = D + rng.randint(0, 4)
+        outer = (n[1] - 1) * inner + D + rng.randint(0, 6)
+        out_s, dims = [outer, inner], n
+        if rng.random() < 0.3:
+            out_s, dims = out_s[::-1], n[::-1]
+        in_s = [rng.choice([s, s, s, 0, rng.randint(0, 30)]) for s in out_s]
+        at = 200 + rng.randint(-outer * n[0] - 8, outer * n[0] + 8) if rng.random() < 0.9 else 200
+        exact = all(k == 1 or a in (0, b) for k, a, b in zip(dims, in_s, out_s))
+        same = at == 200 and all(k == 1 or a == b for k, a, b in zip(dims, in_s, out_s))
+        A, B = places(200, out_s, dims, D), places(at, in_s, dims, D)
+        want = not same and (bool(A & B) if exact else max(A) >= min(B) and max(B) >= min(A))
+        got = bool(fn(400, two(*out_s), 2 * at, two(*in_s), two(*dims), D))
+        assert got == want, (out_s, in_s, dims, D, at)
+        assert got or same or not A & B
+        seen[got, exact] += 1
+    assert min(seen.values()) > 1000
+    far = two(2 ** 62, 2 ** 62)  # extents beyond 64 bits
+    assert fn(400, far, 2 ** 62, two(0, 1), two(9, 9), 8) == 1 and fn(400, far, 200, two(0, 1), two(9, 9), 8) == 0
+
+
+ROW = 2 * 64  # bytes of a row of the calls below
+
+
+@pytest.mark.parametrize("change", [
+    dict(sum=P + ROW), dict(sum=P - ROW), dict(sum=P + 3 * ROW), dict(sum=P + 16), dict(ldx=72, ldr=64, sum=P + 16),
+    dict(residual=2 * P, sum=2 * P + ROW), dict(X=4 * P, residual=2 * P, sum=2 * P + 3 * ROW - 16)])
+def test_norm_refuses_a_sum_over_other_rows(lib, change):
+    assert norm(**dict(BOTH, **change)) == 1
+
+
+@pytest.mark.parametrize("change", [
+    {}, dict(sum=P + 4 * ROW), dict(sum=P - 4 * ROW), dict(residual=8 * P, sum=8 * P),
+    dict(ldx=128, ldr=128, lds=128, sum=P + ROW), dict(M=1, sum=P + ROW), dict(M=1, lds=128), dict(residual=P + ROW, sum=8 * P)])
+def test_norm_takes_a_sum_beside_its_inputs(lib, change):
+    assert norm(**dict(BOTH, **change)) not in (0, 1, 2, 3)  # (there is no device here)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(residual=P + 64), 1), (dict(residual=P - 64), 1), (dict(residual=P + 2), 1), (dict(residual=P + 2, ldr=33), 1),
+    (dict(residual=P + 32, act=2, ldr=16), 1), (dict(residual=P + 3 * 64 + 62), 1),
+    (dict(residual=P), None), (dict(residual=P + 4 * 64), None), (dict(residual=P - 4 * 64), None),
+    (dict(residual=P + 64, M=1), None), (dict(residual=P + 4 * 32, act=2, ldr=16), None)])
+def test_product_refuses_a_residual_over_other_rows(lib, change, code):
+    got = post(**dict(dict(ldr=32), **change))
+    assert got == code if code else got not in (0, 1, 2, 3)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(out=P + 256), 1), (dict(out=P + 128), 1), (dict(out=P - 2), 1), (dict(out=P + 2 * 512 - 2), 1), (dict(ts=0, hs=64, out=P + 128), 1),
+    (dict(ts=64, hs=256, out=P + 256), 1), (dict(ts=136), 1),
+    ({}, None), (dict(out=P + 2 * 512), None), (dict(ts=256, ots=256, out=P + 256), None), (dict(ts=256, ots=256, out=P + 128), 1),
+    (dict(ts=256, ots=256, hs=0, out=P + 128), None), (dict(T=1, ts=8, out=P + 256), None)])
+def test_rope_refuses_an_out_over_other_heads(lib, change, code):
+    got = turn(**change)
+    assert got == code if code else got not in (0, 1, 2, 3)

@@ -340,3 +340,23 @@ def test_empty():
     assert q.codes.shape == (0, 64)
     q, s = mx.rms_norm(torch.zeros((0, 64), dtype=F16, device=DEV), None, torch.zeros((0, 64), dtype=F16, device=DEV))
     assert s.shape == (0, 64)
+
+
+def test_sums_over_other_rows_are_refused():
+    """Nothing is launched, and what lies there stays; a sum beside its inputs, in the same rows, is taken."""
+    g = gen(21)
+    M, K = 70, 640
+    space = rows_of(g, M + 8, 3 * K, BF16)
+    before = space.clone()
+    X, R = space[:M, :K], space[:M, K:2 * K]
+    for out in (space[1:M + 1, :K], space[8:, :K], space[3:M + 3, K:2 * K], space[:M, 8:K + 8], space[:M, K - 8:2 * K - 8],
+                space.view(-1)[K:K + M * (K + 8)].view(M, K + 8)[:, :K]):
+        with pytest.raises(clq.ClqError):
+            mx.rms_norm(X, None, R, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(space, before)
+    want, s = mx.rms_norm(X.contiguous(), None, R.contiguous())
+    for out in (space[8:, 2 * K:], space[:M, 2 * K:], space[:M, K:2 * K]):
+        q, h = mx.rms_norm(X, None, R, out=out)
+        assert h is out and torch.equal(h, s) and torch.equal(q.codes, want.codes)
+        space.copy_(before)

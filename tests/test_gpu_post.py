@@ -320,6 +320,21 @@ def test_shared_tiles_not_finite_in_every_format(fmt, M, K, N, tile):
 
 
 
+def test_residuals_over_other_rows_are_refused():
+    g = gen(22)
+    x, w, bias = operands(g, 100, 160, 144, "block32_e4m3", BF16, True)
+    space = torch.randn((109, 144), generator=g, device=DEV).to(BF16)
+    before = space.clone()
+    Y = space[:100]
+    for R in (space[1:101], space[8:108], space.view(-1)[1:1 + 100 * 144].view(100, 144), space.view(-1)[8:8 + 100 * 152].view(100, 152)[:, :144]):
+        with pytest.raises(clq.ClqError):
+            mx.linear(x, w, bias, Y=Y, residual=R)
+    torch.cuda.synchronize()
+    assert torch.equal(space, before)
+    wide = torch.cat((space, space), 1)[:100]
+    assert torch.equal(mx.linear(x, w, bias, Y=Y, residual=wide[:, 144:]), mx.linear(x, w, bias, residual=before[:100]))
+
+
 # ------------------------------------------------------------- the three in a row --
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [F16, BF16])
