@@ -182,7 +182,7 @@ __device__ __forceinline__ void post_tiles(Bars& bars, uint8_t* smem, const CUte
     const int n0 = T.n0 + channel0;
     next.row = T.row0;
     next.rows = n0 < g.N ? T.rows : 0;
-    next.x = n0 * OUT / EPI_COLS;
+    next.x = first_column(n0, EPI == EPI_GATED);
     next.down = C::OV > 0 && (tc & 1) == 0;
     next.first = static_cast<unsigned>(part + tc) % PARTS;
 #pragma unroll

@@ -17,6 +17,10 @@ struct TileShape {
   int split = 1;  // CTAs that share its K steps
 };
 
+// The first column of Y of the channels from n0 on (a multiple of 32), two of which are one column if
+// they are `gated`.
+constexpr int first_column(int n0, bool gated) { return gated ? n0 / 2 : n0; }
+
 // At most so many: a cluster's eight; more rows are better cut into more tiles.
 constexpr int max_split(int nt) { return nt <= 32 ? 8 : nt <= 64 ? 4 : 1; }
 

@@ -374,3 +374,21 @@ def test_product_refuses_a_residual_over_other_rows(lib, change, code):
 def test_rope_refuses_an_out_over_other_heads(lib, change, code):
     got = turn(**change)
     assert got == code if code else got not in (0, 1, 2, 3)
+
+
+def test_columns_of_many_channels(tmp_path):
+    """Exact for every number of channels that the calls take (an overflow would end the program)."""
+    program = """
+#include "mx_tiles.h"
+#include <cstdio>
+int main() {
+  for (int n0 : {0, 32, 1 << 26, (1 << 27) + 32, (1 << 30) - 32})
+    std::printf("%d %d ", clq::mx::first_column(n0, false), clq::mx::first_column(n0, true));
+}
+"""
+    exe = str(tmp_path / "columns")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-ftrapv", "-I", build.CSRC, "-x", "c++", "-", "-o", exe], input=program,
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    out = subprocess.run([exe], capture_output=True, text=True, check=True).stdout
+    assert [int(v) for v in out.split()] == [v for n in (0, 32, 2 ** 26, 2 ** 27 + 32, 2 ** 30 - 32) for v in (n, n // 2)]

@@ -335,6 +335,28 @@ def test_residuals_over_other_rows_are_refused():
     assert torch.equal(mx.linear(x, w, bias, Y=Y, residual=wide[:, 144:]), mx.linear(x, w, bias, residual=before[:100]))
 
 
+@pytest.mark.parametrize("M", [1, 40])
+@pytest.mark.parametrize("post", [None, "gelu", "swiglu"])
+def test_many_channels(M, post):
+    """More than 2^27 channels: the columns of parts of them."""
+    N, K = 2 ** 27 + 160, 32
+    g = gen(31)
+    codes = torch.randint(0, 0x70, (N, K), generator=g, device=DEV, dtype=torch.uint8)
+    scales = torch.randint(118, 122, mx.scale_shape(N, K, "block32_e4m3"), generator=g, device=DEV, dtype=torch.uint8)
+    w = mx.MXTensor(codes, scales, None, "block32_e4m3")
+    x = mx.quantize(rows_of(g, M, K, BF16), "block32_e4m3")
+    columns = N // 2 if post == "swiglu" else N
+    R = torch.empty((M, columns), dtype=BF16, device=DEV).random_(-100, 100, generator=g)
+    Y = mx.linear(x, w, post=post, residual=R)
+    for n0 in (0, 2 ** 26 - 1024, 2 ** 26, 2 ** 27 - 1024, 2 ** 27):
+        n1 = min(n0 + 2048, N)
+        part = mx.MXTensor(codes[n0:n1], scales[n0 // 128:-(-n1 // 128)], None, "block32_e4m3")
+        c0, c1 = (n0 // 2, n1 // 2) if post == "swiglu" else (n0, n1)
+        want = mx.linear(x, part, post=post, residual=R[:, c0:c1])
+        assert torch.equal(Y[:, c0:c1], want)
+        check(want, x, part, None, 1, post, R[:, c0:c1])
+
+
 # ------------------------------------------------------------- the three in a row --
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [F16, BF16])
