@@ -134,8 +134,9 @@ clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K,
 /*
  * clq_mx_linear with an activation and a residual behind it:
  *   Y[i][n] = out_dtype(act(sum_k x[i][k] w[n][k] / b + bias[n]) + residual[i][n]),
- * in fp32 up to the one rounding.  GELU is within 2^-18 of itself and 2^-22 |x| here, SWIGLU as
- * stated at clq_mx_act.  SWIGLU: N % 16 == 0, channels 16 j .. + 7 are the gate and
+ * in fp32 up to the one rounding.  GELU is within 2^-18 of itself and 2^-22 |x| here, and within
+ * 2^-13 of itself to x = -6, 2^-10 to x = -12.9 and 2^-122 behind it (0, and 0 of minus infinity);
+ * SWIGLU as stated at clq_mx_act.  SWIGLU: N % 16 == 0, channels 16 j .. + 7 are the gate and
  * 16 j + 8 .. + 15 the up half of columns 8 j .. + 7, Y and residual have N / 2 columns.
  * residual: device [M][ldr] of `dtype`, 2-byte aligned, any ldr >= its columns, or NULL; it may
  * be Y itself (ldr then Y's columns); one that meets Y otherwise is refused.  The order

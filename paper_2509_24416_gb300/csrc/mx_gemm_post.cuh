@@ -14,8 +14,8 @@
 //
 // What bounds it is the epilogue warps' instructions where K is short (a value costs 5 in the plain
 // epilogue, 9 with a residual, 14 with GELU), the MMAs where it is long.  Measured, us, E4M3
-// 8192 x 1152 -> 3456 with GELU / a residual / both, plain 28: twelve warps of 128 registers 31 /
-// 32 / 34; eight, all blocks of a tile unrolled, 43 / 36 / 53 (fetching instructions); sixteen of
+// 8192 x 1152 -> 3456 with GELU / a residual / both, plain 28: 32 / 32 / 37.  With a shorter GELU (the
+// logistic one named at gelu_post): twelve warps of 128 registers 31 / 32 / 34; eight, all blocks of a tile unrolled, 43 / 36 / 53 (fetching instructions); sixteen of
 // 96 registers, with a stage less of operands, 33 / 36 / 37; sixteen, blocks of 16 rows, 36 / 36 /
 // 42; with one staging buffer 37 / 45 / 51 (a store's read waits behind the operands' copies);
 // residuals by loads of the lanes and results by their stores 46 / 50 / 61; residuals prefetched
@@ -58,21 +58,33 @@ __device__ __forceinline__ float2 add2(float2 v, uint32_t r) {
                                    Num<T>::to_f(static_cast<uint16_t>(r >> 16))));
 }
 
-// GELU as x / (1 + 2^(-x P(x^2))): x P(x^2) = log2(Phi(x) / Phi(-x)), Phi the normal distribution
-// function, is odd and smooth, so that P of degree 5 (iteratively reweighted least squares up to
-// |x| = 5, constant behind it) gives GELU within 2^-18 of itself and 2^-22 |x|, with 7 1/2
-// instructions a value where gelu_fast has 12 1/2; infinity is its own value, minus infinity NaN.
+__device__ __forceinline__ float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+
+// GELU of an accumulator, which may be anything, as max(x, 0) - |x| 2^N(-|x|): N, log2 of the normal
+// distribution function, of degree 8 (iteratively reweighted least squares down to -13).  Within 2^-18 of
+// itself and 2^-22 |x|, and, so that a 16-bit result has its digits far down the negative side too, within 2^-13
+// of itself to x = -6 and 2^-10 to -12.9 (a quarter of half a step of fp16, which ends there, and of bf16) and
+// 2^-122 behind that.  Infinity is its own value, minus infinity 0, NaN NaN.
+// a = |x| / 16, at most 1 (two operations in one instruction of the multiply-add pipe; by minima 33.1 us, 72.3, for 32.5,
+// 69.2), 16 in the exponential.  Eight instructions a value.  Measured, us, E4M3 8192 x 1152 -> 3456 / blocks of
+// 32 16384 x 1152 -> 4608: this 32.5 / 69.2; gelu_fast with the same ends, 12 1/2 instructions, 37.4 / 84.7; a logistic form
+// that is exact to 2^-22 |x| alone, five times too large at x = -5.5, 31.7 / 67.6.
 __device__ __forceinline__ float2 gelu_post(float2 x) {
-  float2 u = __fmul2_rn(x, x);
-  u = make_float2(fminf(u.x, 25.f), fminf(u.y, 25.f));
-  float2 p = __ffma2_rn(u, both(1.7400531e-07f), both(-8.374469e-06f));
-  p = __ffma2_rn(p, u, both(1.391742e-04f));
-  p = __ffma2_rn(p, u, both(1.5648092e-04f));
-  p = __ffma2_rn(p, u, both(-0.10491368f));
-  p = __ffma2_rn(p, u, both(-2.302181f));
-  p = __fmul2_rn(p, x);
-  const float2 d = __fadd2_rn(make_float2(exp2_fast(p.x), exp2_fast(p.y)), both(1.f));
-  return __fmul2_rn(x, make_float2(rcp_fast(d.x), rcp_fast(d.y)));
+  const float2 a = make_float2(__saturatef(fabsf(x.x) * 0.0625f), __saturatef(fabsf(x.y) * 0.0625f));
+  float2 p = __ffma2_rn(a, both(206.0473175048828f), both(-734.8352661132812f));
+  p = __ffma2_rn(p, a, both(1125.03515625f));
+  p = __ffma2_rn(p, a, both(-982.8634033203125f));
+  p = __ffma2_rn(p, a, both(554.6920776367188f));
+  p = __ffma2_rn(p, a, both(-220.39712524414062f));
+  p = __ffma2_rn(p, a, both(-117.40802764892578f));
+  p = __ffma2_rn(p, a, both(-18.419126510620117f));
+  p = __ffma2_rn(p, a, both(3.0000009536743164f));
+  const float2 h = make_float2(exp2_fast(p.x), exp2_fast(p.y));
+  return make_float2(__fmaf_rn(-a.x, h.x, max_nan(x.x, 0.f)), __fmaf_rn(-a.y, h.y, max_nan(x.y, 0.f)));
 }
 
 // A block of the residual (`rows` of its rows from row0, columns col0 .. + W - 1) into a staging

@@ -357,6 +357,57 @@ def test_many_channels(M, post):
         check(want, x, part, None, 1, post, R[:, c0:c1])
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_gelu_of_every_value(fmt, dtype):
+    """Every finite value of the type as a channel's bias beside a product of 0: relative to itself wherever the type
+    holds it, on the far negative side too."""
+    v = torch.arange(-32768, 32768, device=DEV, dtype=torch.int16).view(dtype)
+    v = v[torch.isfinite(v)]
+    v = torch.cat((v, v[:-v.numel() % 16]))
+    x = mx.quantize(torch.zeros((3, 32), dtype=dtype, device=DEV), fmt)
+    w = mx.quantize(torch.zeros((v.numel(), 32), dtype=dtype, device=DEV), fmt)
+    Y = mx.linear(x, w, v, dtype=dtype, post="gelu")
+    d = v.double()
+    want = d * 0.5 * torch.special.erfc(-d / 2 ** 0.5)
+    # of GELU 2^-13 of itself to -6, 2^-10 behind it, nothing below 2^-122; then half a step
+    own = torch.where(d >= -6, 2.0 ** -13, 2.0 ** -10)
+    room = (ref.HALF_STEP[dtype] * (1 + 2.0 ** -8) + own) * want.abs() + ref.TINY[dtype] + 2.0 ** -122
+    assert ((Y.double() - want).abs() <= room).all()
+    near = (d >= -3) & (d <= 3)
+    room = (ref.HALF_STEP[dtype] * (1 + 2.0 ** -10) + 2.0 ** -18) * want.abs() + ref.TINY[dtype] + 2.0 ** -22 * d.abs()
+    assert ((Y.double() - want).abs() <= room)[:, near].all()
+
+
+def test_gelu_in_front_and_behind():
+    """The same activation behind a product and in front of the next one's quantization."""
+    v = torch.linspace(-14, 6, 4096, device=DEV).to(BF16)
+    x = mx.quantize(torch.zeros((32, 32), dtype=BF16, device=DEV), "block32_e4m3")
+    w = mx.quantize(torch.zeros((4096, 32), dtype=BF16, device=DEV), "block32_e4m3")
+    Y = mx.linear(x, w, v, post="gelu")
+    behind = mx.quantize(Y, "block32_e4m3")
+    ahead = mx.quantize(v[None].expand(32, 4096).contiguous(), "block32_e4m3", act="gelu")
+    a, b = ref.values(behind), ref.values(ahead)
+    # each half a step of E4M3 (2^-4) from the same value, one of them behind bf16's rounding (2^-8) and within 2^-10
+    # of itself and 2^-122; steps of a block's smallest numbers are 2^-9 of its scale
+    scale = torch.maximum(ref.scales(behind), ref.scales(ahead)).repeat_interleave(32, 1)
+    assert ((a - b).abs() <= (2 * 2.0 ** -4 + 2.0 ** -7) * torch.maximum(a.abs(), b.abs()) + 2.0 ** -9 * scale + 2.0 ** -122).all()
+
+
+def test_gelu_of_infinities():
+    """Biases of infinities and NaN: the first its own value, minus infinity 0, NaN NaN; with a residual its own."""
+    v = torch.tensor([float("inf"), float("-inf"), float("nan"), 1.0] * 4, device=DEV)
+    for fmt in FORMATS:
+        for dtype in (F16, BF16):
+            x = mx.quantize(torch.zeros((5, 64), dtype=dtype, device=DEV), fmt)
+            w = mx.quantize(torch.zeros((16, 64), dtype=dtype, device=DEV), fmt)
+            Y = mx.linear(x, w, v.to(dtype), dtype=dtype, post="gelu").float()
+            assert (Y[:, 0] == float("inf")).all() and (Y[:, 1] == 0).all() and Y[:, 2].isnan().all() and (Y[:, 3] > 0.8).all()
+            R = torch.full((5, 16), 2.0, dtype=dtype, device=DEV)
+            Y = mx.linear(x, w, v.to(dtype), dtype=dtype, post="gelu", residual=R).float()
+            assert (Y[:, 0] == float("inf")).all() and (Y[:, 1] == 2).all() and Y[:, 2].isnan().all()
+
+
 # ------------------------------------------------------------- the three in a row --
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [F16, BF16])
