@@ -2,7 +2,9 @@
 
 As ``clq``: ``clq_mx_*`` functions with the C names and arguments, tensor helpers that
 allocate their outputs with torch on the call's stream and raise ``clq.ClqError`` on a
-non-zero status, and the layers made of them.  Every step runs in libclq.so.
+non-zero status, and the layers made of them.  Every step runs in libclq.so.  A call's
+``stream`` orders the call's own work: inputs that another stream still works on are the
+caller's to wait for (``stream.wait_stream``).
 
 * ``quantize`` / ``dequantize``: rows <-> ``MXTensor`` (E2M1 or E4M3 codes, block scales), with
   the layer's swap and rotation or an activation in front; ``rms_norm``: the same behind a

@@ -360,3 +360,52 @@ def test_sums_over_other_rows_are_refused():
         q, h = mx.rms_norm(X, None, R, out=out)
         assert h is out and torch.equal(h, s) and torch.equal(q.codes, want.codes)
         space.copy_(before)
+
+
+def same(a, b):
+    """The same numbers, NaN in the same places."""
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(0, 1e30, -1e30), b.nan_to_num(0, 1e30, -1e30))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,K,b", [(2, 32, 32), (7, 96, 16), (65, 1152, 64), (9, 512, 256), (3, 16384, 256), (12, 160, 1), (200, 4608, 8),
+                                   (2000, 576, 64)] + MANY)
+@pytest.mark.parametrize("place", ["new", "residual", "input"])
+def test_swapped_sums(fmt, dtype, M, K, b, place):
+    """The stored sum beside a swap, by its definition, with infinities and NaN in it; rows that are alone in a block, of
+    whole warps, and that share warps."""
+    g = gen(M + K + b)
+    X, R = rows_of(g, M, K, dtype), rows_of(g, M, K, dtype, 3.0)
+    X[M // 2, 3], X[M // 3, K - 1], R[M - 1, K // 2] = float("nan"), float("inf"), float("-inf")
+    R[M // 3, K - 1] = float("-inf")
+    want = (X.float() + R.float()).to(dtype)
+    out = {"new": None, "residual": R, "input": X}[place]
+    q, s = mx.rms_norm(X, None, R, fmt=fmt, perm=perm_of(g, K), b=b, out=out)
+    assert out is None or s is out
+    assert same(s, want) and want.isnan().any()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,K", [(1, 32), (33, 96), (300, 512), (700, 1152), (2, 16384), (470, 8224)])
+def test_sums(fmt, M, K):
+    """The same without a swap."""
+    g = gen(M + K)
+    X, R = rows_of(g, M, K, F16), rows_of(g, M, K, F16, 3.0)
+    X[M // 2, 3], R[M - 1, K // 2] = float("nan"), float("inf")
+    assert same(mx.rms_norm(X, None, R, fmt=fmt)[1], (X.float() + R.float()).to(F16))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_on_another_stream(fmt):
+    """On another stream, which has waited for the inputs, beside work on the first."""
+    g = gen(25)
+    X, R = rows_of(g, 300, 640, BF16), rows_of(g, 300, 640, BF16)
+    perm = perm_of(g, 640)
+    want, s = mx.rms_norm(X, None, R, fmt=fmt, perm=perm, b=64)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [mx.rms_norm(X, None, R, fmt=fmt, perm=perm, b=64, stream=side) for _ in range(8)]
+    torch.cuda.current_stream().wait_stream(side)
+    for q, t in got:
+        assert torch.equal(q.codes, want.codes) and torch.equal(ref.scale_bytes(q), ref.scale_bytes(want)) and torch.equal(t, s)

@@ -408,6 +408,19 @@ def test_gelu_of_infinities():
             assert (Y[:, 0] == float("inf")).all() and (Y[:, 1] == 2).all() and Y[:, 2].isnan().all()
 
 
+def test_on_another_stream():
+    """A layer on another stream, which has waited for the inputs."""
+    g = gen(26)
+    layer = mx.MXLinear.from_weight(rows_of(g, 1152, 640, BF16, 0.1), "block32_e4m3")
+    X, R = rows_of(g, 3000, 640, BF16), rows_of(g, 3000, 1152, BF16)
+    want = layer(X, post="gelu", residual=R)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [layer(X, post="gelu", residual=R, stream=side) for _ in range(8)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(y, want) for y in got)
+
+
 # ------------------------------------------------------------- the three in a row --
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [F16, BF16])
