@@ -25,6 +25,7 @@ FORMATS = {"block32": BLOCK32, "block16": BLOCK16, "block32_e4m3": BLOCK32_E4M3}
 ACTS = {"none": 0, None: 0, "gelu": 1, "swiglu": 2}
 SCORING = {"softmax": 0, "sigmoid": 1}
 DTYPES = {torch.float16: clq.CLQ_F16, torch.bfloat16: clq.CLQ_BF16}
+_INT32 = 0x7FFFFFFF  # (ctypes cuts what is larger)
 CLQ_F32 = 2
 
 _P, _I, _Z, _F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
@@ -174,6 +175,8 @@ class MXTensor:
 
     def __init__(self, codes, scales, row_scale=None, fmt="block32"):
         lead, rows, K = codes.shape[:-2], codes.shape[-2], _code_width(fmt) * codes.shape[-1]
+        if rows > _INT32:
+            raise ValueError("the number of rows is a 32-bit number, got %d" % rows)
         if len(lead) > 1 or tuple(scales.shape) != tuple(lead) + scale_shape(rows, K, fmt):
             raise ValueError("scales of shape %s do not belong to codes of shape %s"
                              % (tuple(scales.shape), tuple(codes.shape)))
@@ -234,6 +237,9 @@ def _row_input(X, act, perm):
     _on(perm, torch.int32, X.device, "perm")
     if perm is not None and perm.numel() != K:
         raise ValueError("perm must have %d entries" % K)
+    if X.shape[0] > _INT32 or (X.shape[0] > 1 and X.stride(0) > _INT32):
+        raise ValueError("rows and their stride are 32-bit numbers, got %d rows at a stride of %d"
+                         % (X.shape[0], X.stride(0)))
     return K
 
 
@@ -250,7 +256,7 @@ def quantize(X, fmt="block32", perm=None, b=1, act=None, stream=None):
     _on_gpu(X)
     M = X.shape[0]
     codes, scales, rows = _empty(M, K, fmt, X.device)
-    _check(clq_mx_quantize(_ptr(X), _dt(X), M, K, X.stride(0), _ptr(perm), b, ACTS[act], f,
+    _check(clq_mx_quantize(_ptr(X), _dt(X), M, K, X.stride(0) if M > 1 else X.shape[1], _ptr(perm), b, ACTS[act], f,
                            _ptr(codes), _ptr(scales), _ptr(rows), None, 0, M, _stream(stream)),
            "clq_mx_quantize")
     return MXTensor._made(codes, scales, rows, fmt)
@@ -286,7 +292,7 @@ def _like_rows(t, dtype, rows, columns, name):
     if t is None:
         return 0
     _row_major(t, name)
-    if tuple(t.shape) != (rows, columns) or t.dtype != dtype or t.stride(0) > 0x7FFFFFFF:
+    if tuple(t.shape) != (rows, columns) or t.dtype != dtype or (rows > 1 and t.stride(0) > _INT32):
         raise ValueError("%s must be %s of shape (%d, %d), got %s %s"
                          % (name, dtype, rows, columns, t.dtype, tuple(t.shape)))
     return columns if rows <= 1 else t.stride(0)

@@ -12,7 +12,7 @@ import torch
 
 from . import clq
 from .clq import _check, _dt, _elsewhere, _ptr, _stream, _with_stream
-from .mx import _on_gpu
+from .mx import _INT32, _on_gpu
 
 PAIRS = {"interleaved": 0, "halves": 1}
 _P, _I, _L = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
@@ -110,6 +110,9 @@ class Rope:
                 or (self.axes > 1 and positions.stride(1) != 1)):
             raise ValueError("positions must be int32 of shape (%d, %d) with unit column stride"
                              % (T, self.axes))
+        ld = positions.stride(0) if T > 1 else self.axes
+        if T > _INT32 or H > _INT32 or ld > _INT32:  # (ctypes would cut them)
+            raise ValueError("tokens, heads and the stride of positions are 32-bit numbers, got %d, %d, %d" % (T, H, ld))
         if out is None:
             out = torch.empty((T, H, D), dtype=x.dtype, device=x.device)
         elif (out.shape != x.shape or out.dtype != x.dtype or out.stride(2) != 1
@@ -121,7 +124,7 @@ class Rope:
                              % (sum(sections), self.turns.dtype, tuple(self.turns.shape)))
         _on_gpu(x, positions, out, self.turns)
         _check(clq_rope(_ptr(x), _dt(x), T, H, D, x.stride(0), x.stride(1), _ptr(positions),
-                        positions.stride(0), self.axes, sections, _ptr(self.turns),
+                        ld, self.axes, sections, _ptr(self.turns),
                         self.layout, int(bool(inverse)), _ptr(out), out.stride(0),
                         out.stride(1), _stream(stream)), "clq_rope")
         return out

@@ -392,3 +392,36 @@ int main() {
     assert r.returncode == 0, r.stderr
     out = subprocess.run([exe], capture_output=True, text=True, check=True).stdout
     assert [int(v) for v in out.split()] == [v for n in (0, 32, 2 ** 26, 2 ** 27 + 32, 2 ** 30 - 32) for v in (n, n // 2)]
+
+
+def test_sizes_beyond_32_bits(monkeypatch):
+    """Refused, where ctypes would cut them to what fits; a single row's stride does not count."""
+    seen = []
+    monkeypatch.setattr(mx, "_on_gpu", lambda *t: None)
+    monkeypatch.setattr(rope, "_on_gpu", lambda *t: None)
+    for module, names in ((mx, mx.EXPORTS), (rope, rope.EXPORTS)):
+        monkeypatch.setattr(module, "_stream", lambda s: None)
+        for f in names:
+            if f not in ("clq_mx_scale_bytes", "clq_mx_plan_bytes", "clq_mx_plan_rows"):
+                monkeypatch.setattr(module, f, lambda *a, f=f: seen.append((f, a)) or 0)
+    new = lambda *shape, dtype=H: torch.empty(shape, dtype=dtype, device="meta")
+    far, wide = 2 ** 32 + 64, 2 ** 32 + 5
+    rows = lambda n, stride: new(1).as_strided((n, 64), (stride, 1))
+    long = new(1, 64).expand(wide, 64)
+    r = rope.Rope(64, (16, 24, 24), device="meta")
+    x, p = new(4, 2, 64), new(4, 3, dtype=torch.int32)
+    for bad in (lambda: mx.quantize(rows(4, far)), lambda: mx.quantize(long), lambda: mx.rms_norm(rows(4, far)), lambda: mx.rms_norm(long),
+                lambda: mx.rms_norm(new(4, 64), None, rows(4, far)), lambda: mx.rms_norm(new(4, 64), None, new(4, 64), out=rows(4, far)),
+                lambda: mx.MXTensor(new(wide, 64, dtype=torch.uint8), new(*mx.scale_shape(wide, 64, "block32_e4m3"), dtype=torch.uint8), None,
+                                    "block32_e4m3"),
+                lambda: r(x, new(1, dtype=torch.int32).as_strided((4, 3), (far, 1))),
+                lambda: r(new(1, 2, 64).expand(wide, 2, 64), new(1, 3, dtype=torch.int32).expand(wide, 3)),
+                lambda: r(new(2, 1, 64).expand(2, wide, 64), new(2, 3, dtype=torch.int32))):
+        with pytest.raises(ValueError, match="32-bit|must be"):
+            bad()
+    assert not seen
+    mx.quantize(rows(1, far)), mx.rms_norm(rows(1, far), None, rows(1, far))
+    r(x[:1], new(1, dtype=torch.int32).as_strided((1, 3), (far, 1)))
+    ints = [[v for v in a if isinstance(v, int)] for _, a in seen]
+    assert len(ints) == 3 and all(abs(v) <= 0x7FFFFFFF for call in ints for v in call)
+    assert seen[0][1][4] == 64 and seen[1][1][4] == 64 and seen[1][1][6] == 64 and seen[2][1][8] == 3
