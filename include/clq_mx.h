@@ -123,7 +123,8 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
  * [M][ldr] of `dtype` or NULL; sum: device [M][lds], receives h: with a residual only, and may
  * be X or the residual itself (same rows and stride); other rows or columns of them are refused,
  * and ranges of addresses that meet where the strides differ.  weight: device [K] of `dtype` or NULL
- * (ones).  eps > 0.  X, residual, sum and weight 16-byte aligned, strides % 8 == 0.
+ * (ones).  eps: a normal fp32 number, 2^-126 at least.  X, residual, sum and weight 16-byte
+ * aligned, strides % 8 == 0.
  */
 clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K, int32_t ldx,
                            const void* residual, int32_t ldr, const void* weight, float eps,

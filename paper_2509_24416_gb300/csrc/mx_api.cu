@@ -207,7 +207,8 @@ clq_status clq_mx_rms_norm(const void* X, clq_dtype dtype, int32_t M, int32_t K,
                            const int32_t* perm, int32_t b, clq_mx_format fmt, uint8_t* codes,
                            uint8_t* scales, float* row_scale, void* sum, int32_t lds,
                            void* stream) {
-  if (!valid_dtype(dtype) || !valid_format(fmt) || M < 0 || !(eps > 0.f) || std::isinf(eps) ||
+  // (squares below fp32's normal numbers have lost digits, which only a normal eps outweighs)
+  if (!valid_dtype(dtype) || !valid_format(fmt) || M < 0 || !(eps >= 0x1p-126f) || std::isinf(eps) ||
       (residual == nullptr) != (sum == nullptr))
     return CLQ_ERR_INVALID_ARG;
   const bool both = residual != nullptr;

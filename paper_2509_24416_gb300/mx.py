@@ -344,7 +344,7 @@ def rms_norm(X, weight=None, residual=None, eps=1e-6, fmt="block32_e4m3", perm=N
     """X [M, K] fp16 / bf16 -> MXTensor of norm(X) weight, swapped and rotated as in ``quantize``;
     with a residual [M, K] (MXTensor of norm(h), h), h = X + residual rounded to X's type.
     ``out`` receives h (it may be X or the residual, and does not meet them otherwise); see
-    clq_mx_rms_norm."""
+    clq_mx_rms_norm.  eps: 2^-126 at least."""
     if stream is not None and _elsewhere(stream):
         return _with_stream(stream, rms_norm, X, weight, residual, eps, fmt, perm, b, out)
     f = _format(fmt)

@@ -425,3 +425,9 @@ def test_sizes_beyond_32_bits(monkeypatch):
     ints = [[v for v in a if isinstance(v, int)] for _, a in seen]
     assert len(ints) == 3 and all(abs(v) <= 0x7FFFFFFF for call in ints for v in call)
     assert seen[0][1][4] == 64 and seen[1][1][4] == 64 and seen[1][1][6] == 64 and seen[2][1][8] == 3
+
+
+@pytest.mark.parametrize("eps,taken", [(2.0 ** -149, False), (1e-40, False), (2.0 ** -126 - 2.0 ** -149, False), (2.0 ** -126, True),
+                                       (1e-30, True), (3e38, True)])
+def test_smallest_eps(lib, eps, taken):
+    assert (norm(eps=eps) == 1) != taken

@@ -409,3 +409,17 @@ def test_on_another_stream(fmt):
     torch.cuda.current_stream().wait_stream(side)
     for q, t in got:
         assert torch.equal(q.codes, want.codes) and torch.equal(ref.scale_bytes(q), ref.scale_bytes(want)) and torch.equal(t, s)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-36, 1e-30])
+def test_rows_of_small_values(fmt, eps):
+    """Squares around and below the smallest numbers of fp32, beside the smallest eps; a smaller one is refused."""
+    g = gen(27)
+    sizes = 10.0 ** torch.arange(-38, -12, 0.5, device=DEV, dtype=torch.float64)
+    X = (torch.randn((len(sizes), 1152), generator=g, device=DEV).double() * sizes[:, None]).to(BF16)
+    v = ref.norm(X, None, None, eps, BF16)[1]
+    # a square below 2^-126 is off by 2^-150, so is their mean, of which the root counts half: 2^-25 beside eps
+    ref.check_codes(mx.rms_norm(X, eps=eps, fmt=fmt), v, v.abs() * (NORM_OFF + 2.0 ** -24))
+    with pytest.raises(clq.ClqError):
+        mx.rms_norm(X, eps=2.0 ** -127, fmt=fmt)
