@@ -83,8 +83,8 @@ size_t clq_mx_scale_bytes(int32_t rows, int32_t K, clq_mx_format fmt);
  * values a row (2K for SWIGLU).  perm: device int32 [K] or NULL (no swap); b: order
  * of the block Hadamard rotation, a power of two <= 256 with K % b == 0; 1: none.
  * The rotation is unnormalized, as in clq.h, its stages in ascending order.  codes:
- * device [rows][K / 2]; scales: device, clq_mx_scale_bytes; row_scale: device
- * fp32 [rows], BLOCK16 only (NULL else).  out_rows NULL: rows = M and row i is
+ * device [rows][K / 2], BLOCK32_E4M3 [rows][K]; scales: device, clq_mx_scale_bytes; row_scale:
+ * device fp32 [rows], BLOCK16 only (NULL else).  out_rows NULL: rows = M and row i is
  * written to row i.  Else: device int32 [M][k], row i goes to the k rows
  * out_rows[i][..] (negative: nowhere) of `rows` rows; an index >= rows is not
  * written and reported as CLQ_ERR_DEVICE_INDEX, as is one of perm outside [0, K).
@@ -116,7 +116,8 @@ clq_status clq_mx_linear(const uint8_t* Xq, const uint8_t* Xs, const float* s_x,
 /*
  * Norm and quantization: h = dtype(x + residual) (h = x without one), s = mean of the row's h^2,
  *   v = (h * (1 / sqrt(s + eps))) * weight,
- * then v's swap, rotation and quantization as by clq_mx_quantize.  h is rounded to `dtype`
+ * then v's swap, rotation and quantization as by clq_mx_quantize (codes: device [M][K / 2],
+ * BLOCK32_E4M3 [M][K]; scales: clq_mx_scale_bytes of M rows; row_scale: [M], BLOCK16 only).  h is rounded to `dtype`
  * before anything else, so that what is stored is what is normed; all the rest is fp32 (a sum of
  * squares that fp32 does not hold is taken scaled, so every row of finite values has its norm;
  * a row with an infinity or a NaN has the values that the formula gives).  residual: device

@@ -423,3 +423,34 @@ def test_rows_of_small_values(fmt, eps):
     ref.check_codes(mx.rms_norm(X, eps=eps, fmt=fmt), v, v.abs() * (NORM_OFF + 2.0 ** -24))
     with pytest.raises(clq.ClqError):
         mx.rms_norm(X, eps=2.0 ** -127, fmt=fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,K,swap", [(1, 32, False), (70, 96, False), (70, 96, True), (129, 1184, True), (6601, 1152, True)])
+def test_codes_fill_their_bytes(fmt, M, K, swap):
+    """The C calls write the sizes that their header states, all of the codes and nothing behind any array."""
+    g = gen(M + K)
+    X, R = rows_of(g, M, K, F16), rows_of(g, M, K, F16)
+    perm = perm_of(g, K) if swap else None
+    f, b = mx.FORMATS[fmt], 32 if swap else 1
+    P = lambda t: None if t is None else t.data_ptr()
+    code_bytes, scale_bytes = M * (K if fmt == "block32_e4m3" else K // 2), mx.load().clq_mx_scale_bytes(M, K, f)
+    stream = torch.cuda.current_stream().cuda_stream
+    for call in ("quantize", "norm"):
+        got = []
+        for fill in (0x11, 0xEE):
+            codes = torch.full((code_bytes + 256,), fill, dtype=torch.uint8, device=DEV)
+            scales = torch.full((scale_bytes + 256,), fill, dtype=torch.uint8, device=DEV)
+            rows = torch.full((M + 64,), float(fill), device=DEV) if fmt == "block16" else None
+            total = torch.full((M * K + 64,), float(fill), dtype=F16, device=DEV)
+            if call == "quantize":
+                assert mx.clq_mx_quantize(P(X), 0, M, K, K, P(perm), b, 0, f, P(codes), P(scales), P(rows), None, 0, M, stream) == 0
+            else:
+                assert mx.clq_mx_rms_norm(P(X), 0, M, K, K, P(R), K, None, 1e-6, P(perm), b, f, P(codes), P(scales), P(rows), P(total), K,
+                                          stream) == 0
+                assert (total[M * K:] == fill).all()
+            assert (codes[code_bytes:] == fill).all() and (scales[scale_bytes:] == fill).all()
+            assert rows is None or (rows[M:] == fill).all()
+            got.append((codes[:code_bytes], rows[:M] if rows is not None else codes[:0], total[:M * K] if call == "norm" else codes[:0]))
+        for a, c in zip(*got):
+            assert torch.equal(a, c)
