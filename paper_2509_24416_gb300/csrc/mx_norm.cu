@@ -120,7 +120,9 @@ struct Raw {
 // 4096 x 4096 to 8 bits 37 for 33; four blocks spill, 27 us); 1024 have 64.  Rows of more than 8192
 // values leave a SM one block, whose loads alone do not keep memory busy: with a residual and no swap
 // the row behind the next one is asked into L2 (AHEAD; 4096 x 12288 66 us for 75; elsewhere it costs:
-// 16384 x 4608 93 for 84, 4096 x 12288 without a residual 39 for 35, swapped 110 for 108).
+// 16384 x 4608 93 for 84, 4096 x 12288 without a residual 39 for 35, swapped 110 for 108, and 300 x 12288, whose
+// blocks have no row behind the next one, 5.9 for 5.7).  Without a swap rows take whole warps however short they are:
+// 65536 x 256 with half of the lanes 19 us, 25 with a residual (memory alone 8 and 17), 65536 x 1152 63 and 88 (34, 78).
 template <typename T, int FMT, bool RESIDUAL, bool SWAP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS <= 288 ? 3 : 1) norm_kernel(NormArgs a, int R, int packed) {
   extern __shared__ __align__(16) uint8_t stage_raw[];  // SWAP: two rows of 16 bits for each y

@@ -75,7 +75,8 @@ inline TileShape pick_tile(int rows, int matrices, int N, int K, int sms, bool g
 // Few rows with few channels leave most SMs without a tile, and a tile's K steps then take 0.19 us
 // each, the time of their copies to one SM.  So 2, 4 or 8 CTAs share the K steps of a tile of 32 rows
 // (2 or 4 of one of 64) where what they save is more than the `join`: us of its barriers, the sums on
-// their way and the other epilogue.  Measured, us at 1 / 2 / 4 / 8, E4M3 stored as it is: 1 x
+// their way and the other epilogue.  Measured (with barriers at the CTA's scope; the cluster's, which they
+// need, take 0.1 us more), us at 1 / 2 / 4 / 8, E4M3 stored as it is: 1 x
 // 16384 -> 1024 25.7 / 15.7 / 10.3 / 9.0, 1 x 4608 -> 1152 9.0 / 7.2 / 6.0 / 6.8, 1 x 1152 -> 1152 4.0 /
 // 4.8 / 4.7 / 6.2, 16 x 8192 -> 2048 14.3 / 9.8 / 7.5 / 14.8 (clusters that have to wait for one
 // another), 64 x 4608 -> 1152 9.4 / 8.0 / 7.4, 256 x 4096 -> 1024 8.7 / 7.7 / 8.3; blocks of 16 with
