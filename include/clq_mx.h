@@ -46,6 +46,7 @@
  * Every step, the swap and the rotation among them, is one IEEE fp32 operation in the
  * order written, but for an activation (see clq_mx_act); a value that is exactly 0 has
  * code 0 (not 8, its negative).
+ * ADDRESSES.  An output shares no memory with another argument but where a call says so.
  * VERSION.  clq_version counts the functions of clq.h alone; a library has those of this
  * header if it has clq_mx_scale_bytes.
  */

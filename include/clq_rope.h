@@ -5,7 +5,7 @@
  *
  * Conventions are clq.h's (status codes, device pointers owned by the caller,
  * no allocation, no synchronization, asynchronous on `stream`, arguments
- * checked on the host before anything is launched).
+ * checked on the host before anything is launched); `out` shares no memory with positions or turns.
  *
  * A head of D values has P pairs, 2 P <= D; its other D - 2 P values stay as
  * they are.  Pair p of a token belongs to an axis a(p), the first sections[0]
